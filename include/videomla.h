@@ -395,6 +395,108 @@ int videomla_dense_attend(const videomla_dims* dims, const videomla_window* win,
                           size_t workspace_bytes, const videomla_attend_opts* opts,
                           void* stream);
 
+/*
+ * Paged latent cache: the same latents c_kv and rotated keys k_r, in pages of a pool instead of a ring,
+ * for a batch of sequences of different lengths (rollouts at different frames, forked continuations,
+ * token streams). A sequence is a row of a block table: cached token j sits in page
+ * block_table[s][j / page_tokens], at row j % page_tokens of it. Its absolute position is
+ * first_pos[s] + j: frame position / HW and so on, as for the ring (a grid of 1 x 1 makes every token a
+ * frame of its own: 1-D positions, all rope_pairs on the first axis). Keys are rotated at their
+ * absolute position. Of dims, window_frames and chunk_frames are not used; sink_frames must be 0.
+ *
+ * The new tokens of all sequences lie one after the other in the rows of x, q and out: sequence s has
+ * rows cu_tokens[s] .. cu_tokens[s + 1] - 1, none, one or many, and they are the last of its kv_len[s]
+ * cached tokens. Rows from cu_tokens[n_seqs] on belong to no sequence (a batch padded to a fixed size)
+ * and are left as they are.
+ *
+ *   n_seqs         sequences, 1 .. 4096
+ *   n_tokens       rows of x, q_nope, q_r and out
+ *   page_tokens    tokens per page (any number)
+ *   max_pages      columns of the block table; max_pages * page_tokens <= 2^30
+ *   n_pages        pages of the pool; n_pages * page_tokens < 2^31
+ *   max_new        the largest number of new tokens of a sequence, as far as the caller knows it; 0 =
+ *                  n_tokens. It chooses the kernel, the results hold for any lengths
+ *   mask_block     block-causal mask: a query at absolute position p sees the keys of its own and of
+ *                  earlier blocks, positions below (floor(p / mask_block) + 1) * mask_block (1 = causal,
+ *                  a chunk's tokens = chunk-causal); 0 = every cached token of its sequence
+ *   window_tokens  sliding window: of those, only the last window_tokens positions below that block's
+ *                  end (with mask_block 0: below the sequence's end); 0 = all
+ *   cu_tokens      device int32 [n_seqs + 1], not decreasing
+ *   kv_len         device int32 [n_seqs]
+ *   first_pos      device int64 [n_seqs], >= 0, or NULL (all 0): pages of evicted tokens leave the
+ *                  front of the table and first_pos rises by their tokens
+ *   block_table    device int32 [n_seqs][max_pages]. An entry outside [0, n_pages) is a hole: its
+ *                  tokens are written nowhere and seen by nobody (evicted from the middle, say)
+ *   timer          a caller-owned timer, or NULL (kernels "paged_plan", "paged_absorb", "paged_attend",
+ *                  "paged_out", "paged_cache_write")
+ * The arrays are read by the kernels: a captured graph replays with the lengths, positions and pages
+ * that they hold then. Values out of range are clamped (lengths to what the table can name, offsets to
+ * the rows), so that none of them makes a call leave its buffers. Two rows that name the same place of
+ * the pool in one write leave either of the two; everything else in the pool stays as it is.
+ */
+typedef struct videomla_paged {
+  int32_t n_seqs, n_tokens, page_tokens, max_pages, n_pages, max_new;
+  int64_t mask_block, window_tokens;
+  const int32_t* cu_tokens;
+  const int32_t* kv_len;
+  const int64_t* first_pos;
+  const int32_t* block_table;
+  videomla_timer* timer;
+} videomla_paged;
+
+/*
+ * videomla_paged_cache_write -- videomla_cache_write_prepared for the new tokens of every sequence:
+ * compress, normalize, rotate at the token's absolute position, place into its page.
+ *   x          [n_tokens][d_model]                     bf16
+ *   w_packed   as written by videomla_prepare_write_weights
+ *   kv_norm_w  [d_c] bf16 RMSNorm gain, or NULL for no normalization
+ *   c_kv       [n_pages][page_tokens][d_c]             bf16 pool, written in place
+ *   k_r        [n_pages][page_tokens][d_rope]          bf16 pool of ROTATED keys
+ * New tokens whose index kv_len[s] - (cu_tokens[s + 1] - row) is negative, or whose page is a hole, are
+ * not written. Values and requirements of videomla_cache_write_prepared.
+ */
+int videomla_paged_cache_write(const videomla_dims* dims, const videomla_paged* paged,
+                               const uint16_t* x, const uint16_t* w_packed,
+                               const uint16_t* kv_norm_w, uint16_t* c_kv, uint16_t* k_r,
+                               void* stream);
+
+/* Bytes of device workspace videomla_paged_attend needs (0 if the arguments are invalid or not
+ * supported). The device arrays are not read: their pointers may be NULL here. */
+size_t videomla_paged_attend_workspace_bytes(const videomla_dims* dims, const videomla_paged* paged);
+
+/*
+ * videomla_paged_attend -- videomla_attend for the new tokens of every sequence over its pages (already
+ * written), with the mask above. A query that sees nothing gets zeros.
+ *   q_nope     [n_tokens][n_heads][d_nope]   bf16
+ *   q_r        [n_tokens][n_heads][d_rope]   bf16, unrotated
+ *   w_uk, w_uv as for videomla_attend
+ *   c_kv, k_r  the pools as written by videomla_paged_cache_write
+ *   out        [n_tokens][n_heads][d_v]      bf16
+ *   workspace  device buffer of at least videomla_paged_attend_workspace_bytes() bytes; every call
+ *              writes what it reads there, so that calls ordered on one stream may share one
+ * Arithmetic, shapes and errors of videomla_attend. Results are bitwise reproducible. Infinities and
+ * NaN in tokens that a query does not see do not reach it.
+ */
+int videomla_paged_attend(const videomla_dims* dims, const videomla_paged* paged,
+                          const uint16_t* q_nope, const uint16_t* q_r, const uint16_t* w_uk,
+                          const uint16_t* w_uv, const uint16_t* c_kv, const uint16_t* k_r,
+                          uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * videomla_pages_copy -- copies whole pages inside the pools, in every layer: a forked sequence's own
+ * copy of a partly filled page, the moves of a compaction.
+ *   c_kv       [n_layers][n_pages][page_tokens][d_c]    bf16
+ *   k_r        [n_layers][n_pages][page_tokens][d_rope] bf16
+ *   src, dst   HOST arrays of n_pairs page ids: page src[i] to page dst[i]. They are read before the
+ *              call returns (a captured graph keeps their values)
+ * A page may be the source of several pairs. EINVAL, with nothing enqueued, for an id outside
+ * [0, n_pages), a page that is written twice, or one that is both read and written. Requires
+ * page_tokens * d_c % 8 == 0 and page_tokens * d_rope % 8 == 0. n_pairs 0 does nothing.
+ */
+int videomla_pages_copy(const videomla_dims* dims, int32_t page_tokens, int32_t n_pages,
+                        int32_t n_layers, uint16_t* c_kv, uint16_t* k_r, const int32_t* src,
+                        const int32_t* dst, int32_t n_pairs, void* stream);
+
 /* Slide the window after the last denoising step of a chunk (App. "Chunk-Causal Sliding-Window
  * Attention": each chunk's frames join the window and the oldest frames leave it, first in first
  * out): frame_end += chunk_frames. Host only; the eviction itself is implicit, since the next

@@ -7,6 +7,7 @@ streams; importing it fails if the library has not been built.
 from ._lib import (  # noqa: F401
     EXPORTED,
     AttendOpts,
+    Paged,
     Timer,
     VideomlaError,
     attend,
@@ -23,6 +24,10 @@ from ._lib import (  # noqa: F401
     dense_cache_write,
     layer_weights_bytes,
     make_dims,
+    paged_attend,
+    paged_attend_workspace_bytes,
+    paged_cache_write,
+    pages_copy,
     prepare_layer_weights,
     prepare_write_weights,
     slot_of,

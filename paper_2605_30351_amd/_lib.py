@@ -42,6 +42,8 @@ EXPORTED = (
     "videomla_dense_attend_workspace_bytes", "videomla_dense_attend",
     "videomla_layer_weights_bytes", "videomla_prepare_layer_weights",
     "videomla_attend_layer_workspace_bytes", "videomla_attend_layer",
+    "videomla_paged_cache_write", "videomla_paged_attend_workspace_bytes", "videomla_paged_attend",
+    "videomla_pages_copy",
 )
 
 # the diagnostic build's one extra call (include/videomla_stamps.h)
@@ -77,10 +79,21 @@ class VideomlaAttendOpts(ctypes.Structure):
                 ("query_count", ctypes.c_int32), ("timer", ctypes.c_void_p)]
 
 
+class VideomlaPaged(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("mask_block", ctypes.c_int64), ("window_tokens", ctypes.c_int64),
+                ("cu_tokens", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("first_pos", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("timer", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(VideomlaDims)
 _WP = ctypes.POINTER(VideomlaWindow)
 _OP = ctypes.POINTER(VideomlaAttendOpts)
+_GP = ctypes.POINTER(VideomlaPaged)
 
 _lib.videomla_cache_write.argtypes = [_DP, _WP, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P, _P]
 _lib.videomla_cache_write.restype = ctypes.c_int
@@ -144,6 +157,15 @@ _lib.videomla_attend_layer_workspace_bytes.restype = ctypes.c_size_t
 _lib.videomla_attend_layer.argtypes = [_DP, _WP, ctypes.c_int32, ctypes.c_int32, _P, _P,
                                        ctypes.c_size_t, _P, _P, _P, _P, ctypes.c_size_t, _OP, _P]
 _lib.videomla_attend_layer.restype = ctypes.c_int
+_lib.videomla_paged_cache_write.argtypes = [_DP, _GP, _P, _P, _P, _P, _P, _P]
+_lib.videomla_paged_cache_write.restype = ctypes.c_int
+_lib.videomla_paged_attend_workspace_bytes.argtypes = [_DP, _GP]
+_lib.videomla_paged_attend_workspace_bytes.restype = ctypes.c_size_t
+_lib.videomla_paged_attend.argtypes = [_DP, _GP, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]
+_lib.videomla_paged_attend.restype = ctypes.c_int
+_lib.videomla_pages_copy.argtypes = [_DP, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P,
+                                     ctypes.c_int32, _P]
+_lib.videomla_pages_copy.restype = ctypes.c_int
 if STAMPS:
     _lib.videomla_stamps_attach.argtypes = [_P, ctypes.c_int64]
     _lib.videomla_stamps_attach.restype = ctypes.c_int
@@ -501,6 +523,113 @@ def attend_layer(dims, frame_end: int, batch: int, d_q: int, x, weights, c_kv, k
         _ptr(k_r, "k_r"), _ptr(y, "y"), _ptr(workspace, "workspace", (torch.uint8,)),
         workspace.numel() if workspace is not None else 0,
         ctypes.byref(o) if o is not None else None, _stream(stream)))
+
+
+@dataclasses.dataclass
+class Paged:
+    """videomla_paged: a batch of sequences over a paged cache. cu_tokens [n_seqs + 1] and kv_len
+    [n_seqs] int32, first_pos [n_seqs] int64 or None, block_table [n_seqs][max_pages] int32, all on the
+    device and contiguous; n_tokens the rows of x, q and out. The tensors are read when the kernels run:
+    a program changes their contents from step to step and keeps the object."""
+
+    cu_tokens: torch.Tensor
+    kv_len: torch.Tensor
+    block_table: torch.Tensor
+    n_tokens: int
+    page_tokens: int
+    n_pages: int
+    first_pos: torch.Tensor | None = None
+    max_new: int = 0
+    mask_block: int = 0
+    window_tokens: int = 0
+    timer: Timer | None = None
+
+    def struct(self) -> VideomlaPaged:
+        n = self.kv_len.numel()
+        if self.block_table.dim() != 2 or self.block_table.shape[0] != n:
+            raise ValueError(f"block_table must be [{n}][max_pages], got {tuple(self.block_table.shape)}")
+        _need(self.cu_tokens, "cu_tokens", n + 1)
+        if self.first_pos is not None:
+            _need(self.first_pos, "first_pos", n)
+        i32 = (torch.int32,)
+        return VideomlaPaged(
+            n, int(self.n_tokens), int(self.page_tokens), int(self.block_table.shape[1]),
+            int(self.n_pages), int(self.max_new), int(self.mask_block), int(self.window_tokens),
+            _ptr(self.cu_tokens, "cu_tokens", i32), _ptr(self.kv_len, "kv_len", i32),
+            _ptr(self.first_pos, "first_pos", (torch.int64,)),
+            _ptr(self.block_table, "block_table", i32),
+            self.timer.handle if self.timer is not None else None)
+
+
+def _need_pools(d, p, c_kv, k_r):
+    _need(c_kv, "c_kv", p.n_pages * p.page_tokens * d.d_c)
+    _need(k_r, "k_r", p.n_pages * p.page_tokens * d.d_rope)
+
+
+def paged_cache_write(dims, paged: Paged, x, w_packed, gamma, c_kv, k_r, stream=None):
+    """videomla_paged_cache_write on torch tensors; `w_packed` as for cache_write_prepared."""
+    d, p = make_dims(dims), paged.struct()
+    _need(x, "x", p.n_tokens * d.d_model)
+    _need_pools(d, p, c_kv, k_r)
+    if gamma is not None:
+        _need(gamma, "gamma", d.d_c)
+    nbytes = w_packed.numel() * w_packed.element_size()
+    need = int(_lib.videomla_write_weights_bytes(ctypes.byref(d)))
+    if nbytes < need:
+        raise ValueError(f"w_packed holds {nbytes} bytes, needs {need}")
+    _check(_lib.videomla_paged_cache_write(
+        ctypes.byref(d), ctypes.byref(p), _ptr(x, "x"),
+        _ptr(w_packed, "w_packed", (torch.bfloat16, torch.uint8)), _ptr(gamma, "gamma"),
+        _ptr(c_kv, "c_kv"), _ptr(k_r, "k_r"), _stream(stream)))
+
+
+def paged_attend_workspace_bytes(dims, paged: Paged) -> int:
+    return int(_lib.videomla_paged_attend_workspace_bytes(ctypes.byref(make_dims(dims)),
+                                                          ctypes.byref(paged.struct())))
+
+
+def paged_attend(dims, paged: Paged, q_nope, q_r, w_uk, w_uv, c_kv, k_r, out, workspace, stream=None):
+    """videomla_paged_attend on torch tensors; `workspace` is a uint8 device tensor."""
+    d, p = make_dims(dims), paged.struct()
+    rows = p.n_tokens * d.n_heads
+    _need(q_nope, "q_nope", rows * d.d_nope)
+    _need(q_r, "q_r", rows * d.d_rope)
+    _need(w_uk, "w_uk", d.n_heads * d.d_nope * d.d_c)
+    _need(w_uv, "w_uv", d.n_heads * d.d_v * d.d_c)
+    _need_pools(d, p, c_kv, k_r)
+    _need(out, "out", rows * d.d_v)
+    _check(_lib.videomla_paged_attend(
+        ctypes.byref(d), ctypes.byref(p), _ptr(q_nope, "q_nope"), _ptr(q_r, "q_r"),
+        _ptr(w_uk, "w_uk"), _ptr(w_uv, "w_uv"), _ptr(c_kv, "c_kv"), _ptr(k_r, "k_r"),
+        _ptr(out, "out"), _ptr(workspace, "workspace", (torch.uint8,)),
+        workspace.numel() if workspace is not None else 0, _stream(stream)))
+
+
+def pages_copy(dims, page_tokens: int, c_kv, k_r, src, dst, stream=None):
+    """videomla_pages_copy: page src[i] to page dst[i] in every layer of the pools c_kv
+    [n_layers][n_pages][page_tokens][d_c] and k_r [..][d_rope]; src and dst are int32 host tensors (or
+    anything torch.tensor takes)."""
+    d = make_dims(dims)
+    pairs = []
+    for name, ids in (("src", src), ("dst", dst)):
+        t = ids if isinstance(ids, torch.Tensor) else torch.tensor(ids, dtype=torch.int32)
+        if t.is_cuda:
+            raise ValueError(f"{name} must be a host tensor: the call checks the pairs")
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous int32 tensor")
+        pairs.append(t)
+    src, dst = pairs
+    _need(dst, "dst", src.numel())
+    if c_kv.dim() != 4 or k_r.dim() != 4:
+        raise ValueError("c_kv and k_r must be [n_layers][n_pages][page_tokens][width]")
+    layers, pages = c_kv.shape[:2]
+    if tuple(c_kv.shape) != (layers, pages, page_tokens, d.d_c) or \
+            tuple(k_r.shape) != (layers, pages, page_tokens, d.d_rope):
+        raise ValueError(f"pools {tuple(c_kv.shape)}, {tuple(k_r.shape)} do not hold pages of "
+                         f"{page_tokens} tokens of {d.d_c} and {d.d_rope}")
+    _check(_lib.videomla_pages_copy(
+        ctypes.byref(d), int(page_tokens), int(pages), int(layers), _ptr(c_kv, "c_kv"),
+        _ptr(k_r, "k_r"), src.data_ptr(), dst.data_ptr(), src.numel(), _stream(stream)))
 
 
 def window_advance(dims, frame_end: int) -> int:

@@ -15,6 +15,7 @@
 // its rows.
 #include <type_traits>
 #include "vmla_device.h"
+#include "vmla_paged.h"
 
 namespace vmla {
 namespace {
@@ -38,8 +39,11 @@ template <int DC> struct AbsorbChunk {  // W_UK_h columns staged in LDS per pass
   static constexpr bool STAGE = DCP == CW;
 };
 
-template <int DC, int DR>
-__global__ __launch_bounds__(256) void q_absorb_kernel(const AttendArgs a) {
+// Args = PagedAttendArgs: the tokens are those of several sequences one after the other (batch 1, Nq =
+// all token rows), each at its sequence's own position.
+template <int DC, int DR, class Args>
+__global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
+  constexpr bool PAGED = std::is_same<Args, PagedAttendArgs>::value;
   constexpr int DCP = AbsorbChunk<DC>::DCP;
   constexpr int CW = AbsorbChunk<DC>::CW;  // columns per pass (LDS holds d_nope x CW)
   constexpr int WS = CW + 8;               // LDS row stride (elements)
@@ -90,7 +94,16 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const AttendArgs a) {
   // its position would otherwise be repeated by every lane that rotates one of its pairs)
   __shared__ double qpos[4][3][32];
   if (lane < 32) {
-    const TokenPos tp = rope_pos(a.geo, query_pos(a.geo, min(tok0 + lane, Nq - 1)));
+    TokenPos tp{};
+    if constexpr (PAGED) {
+      const int t = min(tok0 + lane, Nq - 1), s = paged_seq_of(a.pg, t);
+      if (s >= 0) {
+        const PagedSeq q = paged_seq(a.pg, s);
+        paged_pos(a.pg, q.first + q.kv - (q.hi - t), tp.f, tp.y, tp.x);
+      }
+    } else {
+      tp = rope_pos(a.geo, query_pos(a.geo, min(tok0 + lane, Nq - 1)));
+    }
     qpos[wave][0][lane] = (double)tp.f;
     qpos[wave][1][lane] = (double)tp.y;
     qpos[wave][2][lane] = (double)tp.x;
@@ -1187,8 +1200,21 @@ hipError_t launch_q_absorb(const AttendArgs& a, hipStream_t s) {
   const size_t lds = q_absorb_lds_bytes(a.d_c, a.d_rope, a.d_nope);
 #define X(DC, DR)                                                                    \
   if (a.d_c == DC && a.d_rope == DR) {                                               \
-    hipLaunchKernelGGL((q_absorb_kernel<DC, DR>), grid, dim3(256), lds, s, a);       \
+    hipLaunchKernelGGL((q_absorb_kernel<DC, DR, AttendArgs>), grid, dim3(256), lds, s, a); \
     return hipGetLastError();                                                        \
+  }
+  VMLA_LATENT_SHAPES(X)
+#undef X
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s) {
+  const dim3 grid((a.pg.n_tokens + 127) / 128, a.n_heads);
+  const size_t lds = q_absorb_lds_bytes(a.d_c, a.d_rope, a.d_nope);
+#define X(DC, DR)                                                                            \
+  if (a.d_c == DC && a.d_rope == DR) {                                                       \
+    hipLaunchKernelGGL((q_absorb_kernel<DC, DR, PagedAttendArgs>), grid, dim3(256), lds, s, a); \
+    return hipGetLastError();                                                                \
   }
   VMLA_LATENT_SHAPES(X)
 #undef X

@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "vmla_device.h"
+#include "vmla_paged.h"
 
 namespace vmla {
 namespace {
@@ -66,6 +67,46 @@ __device__ __forceinline__ void sum_wave_parts(const float* part, int stride, in
 #pragma unroll
     for (int w = 0; w < MAXW; ++w) tot[tb] += w < n ? v[w][tb] : 0.f;
   }
+}
+
+// The paged write's tokens t0 + lane (lanes below n): absolute positions, and the table entry that names
+// each one's page, loaded without waiting for it. The sequences of the workgroup's rows are walked in
+// order with uniform (scalar) loads, each lane keeping the values of its own: a search per lane would
+// wait for every weight and activation load in flight. `page` is then read when the row is stored.
+struct PagedToken {
+  int32_t index;   // index in the sequence's cached tokens; < 0: not to be written
+  int32_t page;    // page id as the table has it
+  TokenPos pos;
+};
+__device__ __forceinline__ PagedToken paged_token(const PagedGeo& g, int t0, int n, int lane_tok, bool live) {
+  int lo = 0, hi = g.n_seqs;  // the first sequence that ends behind t0
+  while (lo < hi) {
+    const int m = (lo + hi) >> 1;
+    if (paged_read<true>(g.cu, m + 1) > t0) hi = m;
+    else lo = m + 1;
+  }
+  int32_t seq = 0, index = -1;
+  int64_t first = 0;
+  for (int s = lo; s < g.n_seqs; ++s) {
+    const PagedSeq q = paged_seq<true>(g, s);
+    if (q.lo >= t0 + n) break;
+    if (lane_tok >= q.lo && lane_tok < q.hi) {
+      seq = s;
+      index = q.kv - (q.hi - lane_tok);
+      first = q.first;
+    }
+  }
+  PagedToken r;
+  r.index = live ? index : -1;
+  const int32_t at = index < 0 ? 0 : index;
+  r.page = g.table[(int64_t)seq * g.max_pages + page_of(g, at)];
+  paged_pos(g, first + at, r.pos.f, r.pos.y, r.pos.x);
+  return r;
+}
+// The pool row of such a token, -1: none.
+__device__ __forceinline__ int64_t paged_token_row(const PagedGeo& g, const PagedToken& t) {
+  if (t.index < 0 || t.page < 0 || t.page >= g.n_pages) return -1;
+  return (int64_t)t.page * g.page_tokens + (t.index - page_of(g, t.index) * g.page_tokens);
 }
 
 constexpr uint32_t kOneBf16x2 = 0x3F803F80u;  // two bf16 ones: the gain when there is none
@@ -134,8 +175,11 @@ __device__ __forceinline__ int xpos(int b, int t, int cc, int rows_pad) {
 // One wave per 16 OB outputs of d_c + d_rope (OB = 2, or 4 beyond 288 outputs). KPRE (weight
 // k-steps of 32 columns in flight per wave) divides d_model / 32, so the steady-state loop
 // issues its loads unconditionally and the compiler can count the outstanding loads exactly.
-template <int KPRE, int OB>
-__global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(const WriteArgs a) {
+// Args = PagedWriteArgs: the rows are those of several sequences one after the other (batch 1), placed
+// into pages.
+template <int KPRE, int OB, class Args>
+__global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(const Args a) {
+  constexpr bool PAGED = std::is_same<Args, PagedWriteArgs>::value;
   __shared__ __attribute__((aligned(16))) uint16_t xs[kTokTile * kMaxWriteDModel];
   __shared__ float ssq_part[kMaxWaves][kTokTile];
   __shared__ int64_t tok_slot[kTokTile];
@@ -207,7 +251,14 @@ __global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(cons
   // with the pair index uniform across a wave, so that the angle table is read by scalar loads
   // (a per-lane index would turn them into vector loads that wait for every load in flight)
   const int npair = DR / 2;
-  if (lane < ntok) {
+  PagedToken pt{};
+  if constexpr (PAGED) {
+    pt = paged_token(a.pg, (int)g0, ntok, (int)g0 + lane, lane < ntok);
+    for (int pr = wave; pr < npair; pr += nwave) {
+      const f32x2 cs = rope_cos_sin(a.rope, __builtin_amdgcn_readfirstlane(pr), pt.pos);
+      if (lane < ntok) rope_cs[lane][pr] = cs;
+    }
+  } else if (lane < ntok) {
     const int g = (int)g0 + lane;  // batch * chunk_tokens < 2^31 (validated on the host)
     const int b = g / n_tok, n = g - b * n_tok;
     const TokenPos pos = token_pos(a.geo, n);
@@ -290,6 +341,9 @@ __global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(cons
     ss[tb] += __shfl_xor(ss[tb], 32);
     if (q == 0) ssq_part[wave][16 * tb + r] = ss[tb];
   }
+  if constexpr (PAGED) {
+    if (wave == 0 && lane < ntok) tok_slot[lane] = paged_token_row(a.pg, pt);
+  }
   __syncthreads();  // every wave is past its last x read: the tile area is reused below
   VMLA_STAMP(a, kStampWritePacked, 4);
 
@@ -310,6 +364,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(cons
   for (int i = threadIdx.x; i < ntok * cpt; i += nwave * 64) {
     const int t = i / cpt, ch = i - t * cpt;
     const int64_t row = tok_slot[t];
+    if (PAGED && row < 0) continue;
     const u32x4 val = *reinterpret_cast<const u32x4*>(&ot[t * ots + ch * 8]);
     const int o = ch * 8;
     if (o < DC) stg16(a.c_kv + (size_t)row * DC + o, val);
@@ -335,8 +390,9 @@ __global__ __launch_bounds__(kMaxWaves * 64) void cache_write_packed_kernel(cons
 // of squares [waves - 1][16 TB], the ring rows [16 TB] and (cos, sin) [16 TB][d_rope / 2 + 1].
 constexpr int kWideBufs = 3;
 
-template <int KPRE, int TB>
-__global__ __launch_bounds__(512) void cache_write_wide_kernel(const WriteArgs a) {
+template <int KPRE, int TB, class Args>
+__global__ __launch_bounds__(512) void cache_write_wide_kernel(const Args a) {
+  constexpr bool PAGED = std::is_same<Args, PagedWriteArgs>::value;
   constexpr int OB = 2, OPW = 16 * OB;
   constexpr int ROWS = 16 * TB;            // token rows of the x buffers (>= the block's tokens)
   constexpr int PK = KPRE / 2;             // k-steps per phase
@@ -374,12 +430,18 @@ __global__ __launch_bounds__(512) void cache_write_wide_kernel(const WriteArgs a
   // waves while the first phase of x lands: wave w takes the pairs w, w + nwave, .. (a pair index
   // uniform across the wave, so that the angle table is read by scalar loads) and wave 0, a
   // compute wave, the ring rows
+  constexpr int NT = (ROWS + 63) / 64;  // tokens per lane
+  PagedToken pt[PAGED ? NT : 1];
   auto tables = [&]() {
-    constexpr int NT = (ROWS + 63) / 64;  // tokens per lane
     TokenPos pos[NT];
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
       const int t = lane + 64 * k;
+      if constexpr (PAGED) {
+        pt[k] = paged_token(a.pg, (int)g0, ntok, (int)g0 + t, t < ntok);
+        pos[k] = pt[k].pos;
+        continue;
+      }
       const int g = (int)g0 + (t < ntok ? t : ntok - 1);  // < 2^31 (validated on the host)
       const int b = g / n_tok, n = g - b * n_tok;
       pos[k] = token_pos(a.geo, n);
@@ -512,6 +574,13 @@ __global__ __launch_bounds__(512) void cache_write_wide_kernel(const WriteArgs a
       ss += __shfl_xor(ss, 32);
       if (q == 0) ssq_part[wave * ROWS + 16 * tb + r] = ss;
     }
+    if constexpr (PAGED) {
+      if (wave == 0) {
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+          if (lane + 64 * k < ntok) tok_slot[lane + 64 * k] = paged_token_row(a.pg, pt[k]);
+      }
+    }
     __syncthreads();  // every wave is past its last x read: the output tile reuses the buffers
     VMLA_STAMP(a, kStampWriteWide, 13);
     // normalized latents and rotated keys, rounded to bf16, into the tile ot[t][0 .. NO)
@@ -534,6 +603,7 @@ __global__ __launch_bounds__(512) void cache_write_wide_kernel(const WriteArgs a
   for (int i = threadIdx.x; i < ntok * cpt; i += nwave * 64) {
     const int t = i / cpt, ch = i - t * cpt;
     const int64_t row = tok_slot[t];
+    if (PAGED && row < 0) continue;
     const u32x4 val = *reinterpret_cast<const u32x4*>(&ot[t * ots + ch * 8]);
     const int o = ch * 8;
     if (o < DC) stg16(a.c_kv + (size_t)row * DC + o, val);
@@ -762,9 +832,9 @@ size_t cache_write_wide_lds_bytes(int kpre, int tb, int ncw, int npair) {
          rows * (npair + 1) * 8;
 }
 
-template <int KPRE>
-hipError_t launch_wide(const WriteArgs& a, int n_cu, hipStream_t s) {
-  WriteArgs b = a;
+template <int KPRE, class Args>
+hipError_t launch_wide(const Args& a, int n_cu, hipStream_t s) {
+  Args b = a;
   const int64_t M = (int64_t)a.batch * a.geo.chunk_tokens;
   const int64_t per = (M + n_cu - 1) / n_cu;
   b.tok_per_wg = (int)(per > kWideMaxTokens ? kWideMaxTokens : per);
@@ -781,9 +851,9 @@ hipError_t launch_wide(const WriteArgs& a, int n_cu, hipStream_t s) {
     return hipGetLastError();
   };
   switch (tb) {
-    case 3: return go(cache_write_wide_kernel<KPRE, 3>);
-    case 4: return go(cache_write_wide_kernel<KPRE, 4>);
-    default: return go(cache_write_wide_kernel<KPRE, 5>);
+    case 3: return go(cache_write_wide_kernel<KPRE, 3, Args>);
+    case 4: return go(cache_write_wide_kernel<KPRE, 4, Args>);
+    default: return go(cache_write_wide_kernel<KPRE, 5, Args>);
   }
 }
 }  // namespace
@@ -800,10 +870,11 @@ hipError_t launch_pack_write_weights(const WriteArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_cache_write(const WriteArgs& a, hipStream_t s) {
-  if (!a.w_packed) return launch_cache_write_staged(a, s);
+namespace {
+template <class Args>
+hipError_t launch_write_packed(const Args& a, hipStream_t s) {
   if (const int kpre = wide_kpre(a, a.n_cu)) {  // batched calls: the panel once per compute unit
-    return kpre == 12 ? launch_wide<12>(a, a.n_cu, s) : launch_wide<8>(a, a.n_cu, s);
+    return kpre == 12 ? launch_wide<12, Args>(a, a.n_cu, s) : launch_wide<8, Args>(a, a.n_cu, s);
   }
   // validated by the caller: d_model % 64 == 0, d_model <= kMaxWriteDModel, d_c % 16 == 0,
   // d_rope % 8 == 0, d_c + d_rope <= 576, 1 <= tok_per_wg <= 32
@@ -815,18 +886,27 @@ hipError_t launch_cache_write(const WriteArgs& a, hipStream_t s) {
   if (nw > kMaxWaves) return hipErrorInvalidValue;
   if (ob == 2) {
     if (nks % 12 == 0)
-      hipLaunchKernelGGL((cache_write_packed_kernel<12, 2>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cache_write_packed_kernel<12, 2, Args>), grid, block, 0, s, a);
     else if (nks % 8 == 0)
-      hipLaunchKernelGGL((cache_write_packed_kernel<8, 2>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cache_write_packed_kernel<8, 2, Args>), grid, block, 0, s, a);
     else
-      hipLaunchKernelGGL((cache_write_packed_kernel<2, 2>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cache_write_packed_kernel<2, 2, Args>), grid, block, 0, s, a);
   } else {  // 64 outputs per wave: fewer k-steps in flight keep the register count in bounds
     if (nks % 4 == 0)
-      hipLaunchKernelGGL((cache_write_packed_kernel<4, 4>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cache_write_packed_kernel<4, 4, Args>), grid, block, 0, s, a);
     else
-      hipLaunchKernelGGL((cache_write_packed_kernel<2, 4>), grid, block, 0, s, a);
+      hipLaunchKernelGGL((cache_write_packed_kernel<2, 4, Args>), grid, block, 0, s, a);
   }
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_cache_write(const WriteArgs& a, hipStream_t s) {
+  return a.w_packed ? launch_write_packed(a, s) : launch_cache_write_staged(a, s);
+}
+
+hipError_t launch_paged_cache_write(const PagedWriteArgs& a, hipStream_t s) {
+  return launch_write_packed(a, s);
 }
 
 }  // namespace vmla

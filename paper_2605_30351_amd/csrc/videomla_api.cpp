@@ -3,6 +3,7 @@
 // launch, so every error path is reachable without a GPU.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -16,6 +17,7 @@
 #include "videomla_stamps.h"
 #endif
 #include "vmla_internal.h"
+#include "vmla_paged.h"
 
 using namespace vmla;
 
@@ -150,14 +152,17 @@ enum KernelId {
   K_Q_ABSORB = 0, K_LATENT_ATTEND, K_OUT_PROJ, K_ROPE_WINDOW, K_BAL_PREP,
   K_MAT_KV, K_MAT_Q_PREP, K_MAT_ATTEND, K_MAT_MERGE,
   K_DENSE_Q_PREP, K_DENSE_ATTEND, K_DENSE_MERGE,
-  K_Q_DOWN, K_Q_UP, K_LATENT_MERGE, K_OUT_MIX, K_CACHE_WRITE, K_DENSE_CACHE_WRITE, K_COUNT
+  K_Q_DOWN, K_Q_UP, K_LATENT_MERGE, K_OUT_MIX, K_CACHE_WRITE, K_DENSE_CACHE_WRITE,
+  K_PAGED_PLAN, K_PAGED_ABSORB, K_PAGED_ATTEND, K_PAGED_OUT, K_PAGED_CACHE_WRITE, K_COUNT
 };
 const char* kKernelNames[K_COUNT] = {"q_absorb",     "latent_attend", "out_proj",
                                      "rope_window",  "bal_prep",      "mat_kv",
                                      "mat_q_prep",   "mat_attend",    "mat_merge",
                                      "dense_q_prep", "dense_attend",  "dense_merge",
                                      "q_down",       "q_up",          "latent_merge",
-                                     "out_mix",      "cache_write",   "dense_cache_write"};
+                                     "out_mix",      "cache_write",   "dense_cache_write",
+                                     "paged_plan",   "paged_absorb",  "paged_attend",
+                                     "paged_out",    "paged_cache_write"};
 
 int kernel_id(const char* name) {
   for (int k = 0; k < K_COUNT; ++k)
@@ -1014,6 +1019,224 @@ int videomla_attend_layer(const videomla_dims* d, const videomla_window* w, int3
 }
 
 // ---- timers -------------------------------------------------------------------------------------
+
+// ---- paged cache ----------------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+int check_paged(const videomla_dims* d, const videomla_paged* p) {
+  if (int e = check_dims(d)) return e;
+  if (!p) return fail(VIDEOMLA_EINVAL, "paged is NULL");
+  if (d->sink_frames) return fail(VIDEOMLA_EUNSUPPORTED, "the paged cache has no sink mode (sink_frames must be 0)");
+  if (p->n_seqs <= 0 || p->n_tokens <= 0 || p->page_tokens <= 0 || p->max_pages <= 0 || p->n_pages <= 0)
+    return fail(VIDEOMLA_EINVAL, "all sizes in paged must be positive");
+  if (p->max_new < 0 || p->mask_block < 0 || p->window_tokens < 0)
+    return fail(VIDEOMLA_EINVAL, "max_new, mask_block and window_tokens must be >= 0");
+  if (p->n_seqs > kPagedMaxSeqs)
+    return fail(VIDEOMLA_EUNSUPPORTED, "n_seqs must be <= %d, got %d", kPagedMaxSeqs, p->n_seqs);
+  if ((int64_t)p->max_pages * p->page_tokens > (int64_t)1 << 30)
+    return fail(VIDEOMLA_EUNSUPPORTED, "max_pages * page_tokens must be <= 2^30");
+  if ((int64_t)p->n_pages * p->page_tokens >= (int64_t)1 << 31)
+    return fail(VIDEOMLA_EUNSUPPORTED, "n_pages * page_tokens must be < 2^31");
+  return VIDEOMLA_OK;
+}
+
+int check_paged_arrays(const videomla_paged* p) {
+  if (!p->cu_tokens || !p->kv_len || !p->block_table) return fail(VIDEOMLA_EINVAL, "NULL array in paged");
+  if (((reinterpret_cast<uintptr_t>(p->cu_tokens) | reinterpret_cast<uintptr_t>(p->kv_len) |
+        reinterpret_cast<uintptr_t>(p->block_table)) & 3u) ||
+      (reinterpret_cast<uintptr_t>(p->first_pos) & 7u))
+    return fail(VIDEOMLA_EALIGN, "the arrays in paged must be aligned to their elements");
+  return VIDEOMLA_OK;
+}
+
+PagedGeo make_paged_geo(const videomla_dims* d, const videomla_paged* p) {
+  PagedGeo g{};
+  g.cu = p->cu_tokens; g.kv_len = p->kv_len; g.first_pos = p->first_pos; g.table = p->block_table;
+  g.n_seqs = p->n_seqs; g.n_tokens = p->n_tokens; g.page_tokens = p->page_tokens;
+  g.max_pages = p->max_pages; g.n_pages = p->n_pages;
+  g.max_kv = p->max_pages * p->page_tokens;
+  set_page_division(g);
+  g.mask_block = std::min(p->mask_block, kPagedFar);
+  g.window = std::min(p->window_tokens, kPagedFar);
+  g.grid_h = d->grid_h; g.grid_w = d->grid_w;
+  return g;
+}
+
+// Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots, the
+// plan and the row of zeros.
+struct PagedLayout {
+  size_t qcat, o_lat, o_part, ml, zero, head, seq_block, block, first_unit, work, total;
+  int32_t rows, unit, max_blocks, n_wg;
+};
+
+int check_paged_attend_shape(const videomla_dims* d, const videomla_paged* p) {
+  if (int e = check_paged(d, p)) return e;
+  if (int e = check_attend_shape(d)) return e;
+  if ((int64_t)p->n_tokens * d->n_heads >= (int64_t)1 << 31)
+    return fail(VIDEOMLA_EUNSUPPORTED, "n_tokens * n_heads must be < 2^31");
+  return VIDEOMLA_OK;
+}
+
+PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
+  PagedLayout L{};
+  const int64_t rows = (int64_t)p->n_tokens * d->n_heads;
+  const int64_t max_new = p->max_new > 0 && p->max_new < p->n_tokens ? p->max_new : p->n_tokens;
+  paged_attend_shape(d->d_c, d->d_rope, max_new * d->n_heads, &L.rows, &L.unit);
+  // a sequence's last block may be partly filled; sequences without rows have none
+  L.max_blocks = (int32_t)(rows / L.rows + (p->n_seqs < p->n_tokens ? p->n_seqs : p->n_tokens));
+  L.n_wg = device_cu_count();
+  const size_t qk = round_up((size_t)d->d_c + d->d_rope, 16);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t off = at;
+    at += round_up(bytes, 256);
+    return off;
+  };
+  L.qcat = take((size_t)rows * qk * 2);
+  L.o_lat = take((size_t)rows * d->d_c * 2);
+  L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
+  L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);
+  L.zero = take(qk * 2);
+  L.head = take(2 * sizeof(int64_t));
+  L.seq_block = take(((size_t)p->n_seqs + 1) * sizeof(int32_t));
+  L.block = take((size_t)L.max_blocks * sizeof(PagedBlock));
+  L.first_unit = take(((size_t)L.max_blocks + 1) * sizeof(int64_t));
+  L.work = take((size_t)L.n_wg * sizeof(PagedWork));
+  L.total = at;
+  return L;
+}
+
+}  // namespace
+
+extern "C" {
+
+int videomla_paged_cache_write(const videomla_dims* d, const videomla_paged* p, const uint16_t* x,
+                               const uint16_t* w_packed, const uint16_t* kv_norm_w, uint16_t* c_kv,
+                               uint16_t* k_r, void* stream) {
+  if (int e = check_write_dims(d)) return e;
+  if (int e = check_paged(d, p)) return e;
+  if (int e = check_paged_arrays(p)) return e;
+  if (!x || !w_packed || !c_kv || !k_r) return fail(VIDEOMLA_EINVAL, "NULL tensor pointer");
+  if (!aligned16(x) || !aligned16(w_packed) || !aligned16(c_kv) || !aligned16(k_r) ||
+      (kv_norm_w && !aligned16(kv_norm_w)))
+    return fail(VIDEOMLA_EALIGN, "tensor pointers must be 16-byte aligned");
+  PagedWriteArgs a{};
+  a.x = x; a.w_packed = w_packed; a.gamma = kv_norm_w; a.c_kv = c_kv; a.k_r = k_r;
+  a.batch = 1; a.d_model = d->d_model; a.d_c = d->d_c; a.d_rope = d->d_rope;
+  a.eps = d->kv_norm_eps;
+  a.geo.chunk_tokens = p->n_tokens;
+  a.rope = make_rope(d);
+  a.n_cu = device_cu_count();
+  a.tok_per_wg = cache_write_tokens_per_wg(p->n_tokens, a.n_cu);
+  a.pg = make_paged_geo(d, p);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = timed(p->timer, K_PAGED_CACHE_WRITE, s, [&] { return launch_paged_cache_write(a, s); });
+  if (e != hipSuccess) return hip_fail(e, "paged_cache_write");
+  return ok();
+}
+
+size_t videomla_paged_attend_workspace_bytes(const videomla_dims* d, const videomla_paged* p) {
+  if (check_paged_attend_shape(d, p)) return 0;
+  return paged_layout(d, p).total;
+}
+
+int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const uint16_t* q_nope,
+                          const uint16_t* q_r, const uint16_t* w_uk, const uint16_t* w_uv,
+                          const uint16_t* c_kv, const uint16_t* k_r, uint16_t* out, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  if (int e = check_paged_attend_shape(d, p)) return e;
+  if (int e = check_paged_arrays(p)) return e;
+  if (!q_nope || !q_r || !w_uk || !w_uv || !c_kv || !k_r || !out)
+    return fail(VIDEOMLA_EINVAL, "NULL tensor pointer");
+  if (!aligned16(q_nope) || !aligned16(q_r) || !aligned16(w_uk) || !aligned16(w_uv) ||
+      !aligned16(c_kv) || !aligned16(k_r) || !aligned16(out))
+    return fail(VIDEOMLA_EALIGN, "tensor pointers must be 16-byte aligned");
+  const PagedLayout L = paged_layout(d, p);
+  if (int e = check_workspace(workspace, workspace_bytes, L.total)) return e;
+  char* ws = static_cast<char*>(workspace);
+  PagedAttendArgs a{};
+  a.q_nope = q_nope; a.q_r = q_r; a.w_uk = w_uk; a.w_uv = w_uv; a.c_kv = c_kv; a.k_r = k_r; a.out = out;
+  a.qcat = reinterpret_cast<uint16_t*>(ws + L.qcat);
+  a.o_lat = reinterpret_cast<uint16_t*>(ws + L.o_lat);
+  a.o_part = reinterpret_cast<float*>(ws + L.o_part);
+  a.ml_part = reinterpret_cast<float*>(ws + L.ml);
+  a.zero_row = reinterpret_cast<uint16_t*>(ws + L.zero);
+  a.plan.head = reinterpret_cast<int64_t*>(ws + L.head);
+  a.plan.seq_block = reinterpret_cast<int32_t*>(ws + L.seq_block);
+  a.plan.block = reinterpret_cast<PagedBlock*>(ws + L.block);
+  a.plan.first_unit = reinterpret_cast<int64_t*>(ws + L.first_unit);
+  a.plan.work = reinterpret_cast<PagedWork*>(ws + L.work);
+  a.max_blocks = L.max_blocks; a.rows = L.rows; a.unit = L.unit;
+  a.batch = 1; a.n_heads = d->n_heads; a.d_nope = d->d_nope; a.d_rope = d->d_rope;
+  a.d_c = d->d_c; a.d_v = d->d_v;
+  a.dqk_pad = (int32_t)round_up((size_t)d->d_c + d->d_rope, 16);
+  a.n_wg = L.n_wg;
+  a.geo.q_count = p->n_tokens;
+  a.rope = make_rope(d);
+  a.pg = make_paged_geo(d, p);
+  const double scale = d->softmax_scale > 0.f ? (double)d->softmax_scale
+                                              : 1.0 / std::sqrt((double)d->d_nope + d->d_rope);
+  a.qscale = (float)(scale * 1.4426950408889634);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e = timed(p->timer, K_PAGED_PLAN, s, [&] { return launch_paged_plan(a, s); });
+  if (e != hipSuccess) return hip_fail(e, "paged_plan");
+  e = timed(p->timer, K_PAGED_ABSORB, s, [&] { return launch_paged_absorb(a, s); });
+  if (e != hipSuccess) return hip_fail(e, "paged_absorb");
+  e = timed(p->timer, K_PAGED_ATTEND, s, [&] { return launch_paged_attend(a, s); });
+  if (e != hipSuccess) return hip_fail(e, "paged_attend");
+  e = timed(p->timer, K_PAGED_OUT, s, [&] { return launch_paged_out(a, s); });
+  if (e != hipSuccess) return hip_fail(e, "paged_out");
+  return ok();
+}
+
+int videomla_pages_copy(const videomla_dims* d, int32_t page_tokens, int32_t n_pages, int32_t n_layers,
+                        uint16_t* c_kv, uint16_t* k_r, const int32_t* src, const int32_t* dst,
+                        int32_t n_pairs, void* stream) {
+  if (int e = check_dims(d)) return e;
+  if (page_tokens <= 0 || n_pages <= 0 || n_layers <= 0 || n_pairs < 0)
+    return fail(VIDEOMLA_EINVAL, "page_tokens, n_pages and n_layers must be positive, n_pairs >= 0");
+  if (n_layers > 65535) return fail(VIDEOMLA_EUNSUPPORTED, "n_layers must be <= 65535, got %d", n_layers);
+  if ((int64_t)n_pages * page_tokens >= (int64_t)1 << 31)
+    return fail(VIDEOMLA_EUNSUPPORTED, "n_pages * page_tokens must be < 2^31");
+  if ((int64_t)page_tokens * d->d_c % 8 || (int64_t)page_tokens * d->d_rope % 8)
+    return fail(VIDEOMLA_EUNSUPPORTED, "a page of %d tokens is not a whole number of 16-byte pieces", page_tokens);
+  if (!c_kv || !k_r || (n_pairs > 0 && (!src || !dst))) return fail(VIDEOMLA_EINVAL, "NULL pointer");
+  if (!aligned16(c_kv) || !aligned16(k_r)) return fail(VIDEOMLA_EALIGN, "tensor pointers must be 16-byte aligned");
+  try {
+    for (int32_t i = 0; i < n_pairs; ++i)
+      if (src[i] < 0 || src[i] >= n_pages || dst[i] < 0 || dst[i] >= n_pages)
+        return fail(VIDEOMLA_EINVAL, "pair %d: page %d to %d is outside the pool of %d pages", i, src[i], dst[i], n_pages);
+    std::vector<int32_t> written(dst, dst + n_pairs);
+    std::sort(written.begin(), written.end());
+    const auto twice = std::adjacent_find(written.begin(), written.end());
+    if (twice != written.end()) return fail(VIDEOMLA_EINVAL, "page %d is written twice", *twice);
+    for (int32_t i = 0; i < n_pairs; ++i)
+      if (std::binary_search(written.begin(), written.end(), src[i]))
+        return fail(VIDEOMLA_EINVAL, "page %d is both read and written", src[i]);
+  } catch (const std::bad_alloc&) {
+    return fail(VIDEOMLA_EINVAL, "no host memory for the check of %d pairs", n_pairs);
+  }
+  PagesCopyArgs a{};
+  const int64_t tokens = page_tokens;
+  a.pool[0] = c_kv; a.pool[1] = k_r;
+  a.page_bytes[0] = tokens * d->d_c * 2;
+  a.page_bytes[1] = tokens * d->d_rope * 2;
+  for (int k = 0; k < 2; ++k) a.layer_bytes[k] = a.page_bytes[k] * n_pages;
+  a.n_layers = n_layers;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  for (int32_t i = 0; i < n_pairs; i += kCopyPairs) {
+    a.n_pairs = n_pairs - i < kCopyPairs ? n_pairs - i : kCopyPairs;
+    std::copy(src + i, src + i + a.n_pairs, a.src);
+    std::copy(dst + i, dst + i + a.n_pairs, a.dst);
+    const hipError_t e = launch_pages_copy(a, s);
+    if (e != hipSuccess) return hip_fail(e, "pages_copy");
+  }
+  return ok();
+}
+
+// ---- timers ---------------------------------------------------------------------------------------
 
 int videomla_timer_create(videomla_timer** timer) {
   if (!timer) return fail(VIDEOMLA_EINVAL, "NULL timer pointer");
