@@ -16,12 +16,6 @@
 namespace vmla {
 namespace {
 
-constexpr float kNegInf = -__builtin_huge_valf();
-// The running maximum starts at the lowest finite value, not at -inf: a row that has seen nothing yet
-// (and one that never will) then keeps all its exponentials at exp2(-inf) = 0, with no inf - inf.
-constexpr float kLowest = -3.402823466e38f;
-constexpr float kLazyMax = 8.0f;  // the running max is raised when exceeded by more (log2 units)
-
 // D(16x16) += A(16x32) B(32x16). Lane l holds A[l%16][8(l/16) .. +8], B[8(l/16) .. +8][l%16];
 // accumulator element i of lane l is D[4(l/16) + i][l%16].
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -34,20 +28,6 @@ __device__ __forceinline__ void lds_dma4(const int32_t* gptr, uint32_t lds_base)
                :
                : "v"(gptr), "s"(lds_base)
                : "memory", "m0");
-}
-
-// bf16 values with infinities and NaN replaced by zero. In a tile that is masked for some row, a key's
-// probability may be 0 while its latent is not finite, and 0 * NaN would reach the rows that do not see
-// it; a row that does see it has a NaN score, since the latent is part of the key.
-__device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 v) {
-  u32x4 u = as_u32x4(v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = (u[i] & 0x7f80u) == 0x7f80u ? 0u : u[i] & 0xffffu;
-    const uint32_t hi = (u[i] & 0x7f800000u) == 0x7f800000u ? 0u : u[i] & 0xffff0000u;
-    u[i] = lo | hi;
-  }
-  return as_bf16x8(u);
 }
 
 // ---- plan -----------------------------------------------------------------------------------
@@ -137,14 +117,14 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PagedAtt
     PagedWork k{};
     if (w < G) {
       const int64_t u = floor_div((int64_t)w * units, G), u1 = floor_div((int64_t)(w + 1) * units, G);
-      int lo = 0, hi = (int)blocks - 1;  // the last block with first_unit <= u
+      int lo = 0, hi = (int)blocks - 1;  // the last block with first_unit < u1
       while (lo < hi) {
         const int m = (lo + hi + 1) >> 1;
-        if (a.plan.first_unit[m] <= u) lo = m;
+        if (a.plan.first_unit[m] < u1) lo = m;
         else hi = m - 1;
       }
       k.block = lo;
-      k.first = (int32_t)(u - a.plan.first_unit[lo]);
+      k.end = (int32_t)(u1 - a.plan.first_unit[lo]);
       k.n_units = (int32_t)(u1 - u);
     }
     a.plan.work[w] = k;
@@ -180,7 +160,7 @@ struct FewCfg {
     return ((q & 1) << 1) | (q >> 1);
   }
   static_assert(CPR % 16 == 4 || CPR % 16 == 12, "bank spread of the tile rows");
-  static_assert(DC % 16 == 0 && 32 * CPR % 64 == 0 && NDMA + 1 < 64, "tile shape");
+  static_assert(DC % 16 == 0 && 16 * CPR % 64 == 0 && NDMA + 1 < 64, "tile shape");
   static_assert(ROWS * RS * 4 <= 2 * TILE * 2, "a wave's results fit its tile buffers");
 };
 
@@ -199,23 +179,24 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
   const int H = a.n_heads;
   const PagedWork wk = a.plan.work[blockIdx.x];
   int left = __builtin_amdgcn_readfirstlane(wk.n_units);
-  int blk = __builtin_amdgcn_readfirstlane(wk.block), u0 = __builtin_amdgcn_readfirstlane(wk.first);
+  int blk = __builtin_amdgcn_readfirstlane(wk.block), end = __builtin_amdgcn_readfirstlane(wk.end);
 
-  // Load j of a tile fills the chunk slots 64 j .. 64 j + 63; this lane's is row r, logical chunk c
-  int d_row[C::NDMA], d_off[C::NDMA];  // d_off: element offset in the row's c_kv (>= 0) or ~offset in its k_r
+  // Load j of a tile fills the chunk slots 64 j .. 64 j + 63: of this lane's chunk, in bits 0..15 the
+  // offset in its row's c_kv, or (bit 31) k_r (the pad reads k_r again, against zeros in q_cat), in bits
+  // 16..19 the row modulo 16. Half a tile is a whole number of loads, and the other half repeats it.
+  uint32_t d_at[C::NDMA / 2];
 #pragma unroll
-  for (int j = 0; j < C::NDMA; ++j) {
-    const int slot = j * 64 + lane, r = slot / C::CPR, pc = slot % C::CPR;
-    const int c = pc ^ C::swz(r);
-    d_row[j] = r;
-    d_off[j] = c < DC / 8 ? c * 8 : ~(c < (DC + DR) / 8 ? c * 8 - DC : 0);  // (the pad reads k_r again)
+  for (int j = 0; j < C::NDMA / 2; ++j) {
+    const int slot = j * 64 + lane, r = slot / C::CPR, c = (slot % C::CPR) ^ C::swz(r);
+    d_at[j] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : 0x80000000u | (c < (DC + DR) / 8 ? c * 8 - DC : 0));
   }
 
   while (left > 0) {
     const PagedBlock pb = a.plan.block[blk];
     const int seq = __builtin_amdgcn_readfirstlane(pb.seq), row0 = __builtin_amdgcn_readfirstlane(pb.row0);
     const int n_units = __builtin_amdgcn_readfirstlane(pb.n_units);
-    const int take = min(left, n_units - u0);
+    if (end == 0) end = n_units;  // a segment before the workgroup's last ends with its block
+    const int take = min(left, end), u0 = end - take;
     const int key0 = __builtin_amdgcn_readfirstlane(pb.key0) + u0 * C::UNIT + wave * 32;  // this wave's first
     const PagedSeq q = paged_seq<true>(g, seq);
     const int n_rows = (q.hi - q.lo) * H, base = q.kv - (q.hi - q.lo);
@@ -278,10 +259,11 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       const uint32_t lds = lds_addr(&tiles[wave][t & 1][0]);
 #pragma unroll
       for (int j = 0; j < C::NDMA; ++j) {
-        const int32_t r = __shfl(row, d_row[j]);
-        const bool kr = d_off[j] < 0;
+        const uint32_t at = d_at[j % (C::NDMA / 2)];
+        const int32_t r = __shfl(row, (int)(at >> 16 & 15) + (j < C::NDMA / 2 ? 0 : 16));
+        const bool kr = (int32_t)at < 0;
         const uint16_t* p = kr ? a.k_r : a.c_kv;
-        p += (int64_t)r * (kr ? DR : DC) + (kr ? ~d_off[j] : d_off[j]);
+        p += (int64_t)r * (kr ? DR : DC) + (at & 0xffffu);
         lds_dma16(r < 0 ? a.zero_row : p, __builtin_amdgcn_readfirstlane(lds + 1024u * j));
       }
     };
@@ -334,19 +316,19 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
             for (int i = 0; i < 4; ++i) {
               const int k = 16 * kb + 4 * gq + i;
               const bool seen = (there >> k & 1) && k0 + k >= see_b[qb] && k0 + k < see_e[qb];
-              s[qb][kb][i] = seen ? s[qb][kb][i] : kNegInf;
+              s[qb][kb][i] = seen ? s[qb][kb][i] : kMasked;
             }
       }
       float own[QB];
       bool grow = false;
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        own[qb] = kNegInf;
+        own[qb] = kMasked;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) own[qb] = fmaxf(own[qb], s[qb][kb][i]);
-        grow |= own[qb] > m_run[qb] + kLazyMax;
+        grow |= own[qb] > m_run[qb] + kLazyMaxStep;
       }
       if (__builtin_amdgcn_ballot_w64(grow) != 0) {
 #pragma unroll
@@ -422,7 +404,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       }
       if (whole) {
         v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-        *reinterpret_cast<bf16x4*>(a.o_lat + ((int64_t)q.lo * H + row0 + r) * DC + c) = to_bf16x4(v);
+        *reinterpret_cast<f32x4*>(a.o_lat + ((int64_t)q.lo * H + row0 + r) * DC + c) = v;
       } else {
         *reinterpret_cast<f32x4*>(a.o_part + (slot * C::ROWS + r) * DC + c) = v;
         if (c == 0) {
@@ -433,21 +415,23 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
     }
     __syncthreads();  // the buffers are free for the next segment
     left -= take;
-    u0 = 0;
-    ++blk;
+    end = 0;
+    --blk;
   }
 }
 
 // ---- merge and value up-projection -------------------------------------------------------------
 // grid (ceil(n_tokens / TG), H), 256 threads: the latents of TG tokens of one head, merged where their
-// row block was split, rounded to bf16 in LDS, then out^T[v][token] = W_UV_h[v][:] . o_lat[token][:].
+// row block was split, then out^T[v][token] = W_UV_h[v][:] . o_lat[token][:]. The latents go into the
+// product as two bf16 terms (16 bits of fraction): one alone adds a rounding as large as the output's
+// own, 2^-8 of the value, for a product that costs next to nothing here.
 template <int DC, int TG>
 __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a) {
   constexpr int LS = (DC > 32 ? DC : 32) + 8;  // LDS row stride (elements)
   constexpr int KS = (DC + 31) / 32;
   constexpr int C4 = DC / 4;                   // 16-byte chunks of a partial row
   constexpr int SL = 256 / C4 < 16 ? 256 / C4 : 16;  // splits read side by side
-  __shared__ __attribute__((aligned(16))) uint16_t lat[16][LS];
+  __shared__ __attribute__((aligned(16))) uint16_t lat[2][TG][LS];  // o_lat's first and second term
   __shared__ f32x4 part[SL][C4];
   __shared__ float part_m[SL], part_l[SL];
   __shared__ int32_t tok_row[TG], tok_w0[TG], tok_ns[TG];  // (ns 0: no token of a sequence)
@@ -471,18 +455,33 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
     }
   }
   if constexpr (DC < 32) {
-    for (int i = tid; i < 16 * LS; i += 256) (&lat[0][0])[i] = 0;
+    for (int i = tid; i < 2 * TG * LS; i += 256) (&lat[0][0][0])[i] = 0;
   }
   __syncthreads();
+  auto put = [&](int t, int c4, f32x4 v) {  // chunk c4 of token t's latents
+    const bf16x4 hi = to_bf16x4(v);
+    const f32x4 rest = v - __builtin_convertvector(hi, f32x4);
+    *reinterpret_cast<bf16x4*>(&lat[0][t][c4 * 4]) = hi;
+    *reinterpret_cast<bf16x4*>(&lat[1][t][c4 * 4]) = to_bf16x4(rest);
+  };
 
+  // tokens of unsplit blocks: every load issued before the first is used
+  constexpr int PER = (TG * C4 + 255) / 256;
+  f32x4 whole[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = tid + 256 * i, t = e / C4;
+    if (e < TG * C4 && tok_ns[t] == 1)
+      whole[i] = *reinterpret_cast<const f32x4*>(a.o_lat + ((int64_t)(t0 + t) * H + h) * DC + e % C4 * 4);
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = tid + 256 * i, t = e / C4;
+    if (e < TG * C4 && tok_ns[t] == 1) put(t, e % C4, whole[i]);
+  }
   for (int t = 0; t < TG; ++t) {
     const int ns = tok_ns[t], w0 = tok_w0[t];
-    if (ns == 0) continue;
-    if (ns == 1) {
-      const uint16_t* src = a.o_lat + ((int64_t)(t0 + t) * H + h) * DC;
-      if (tid < DC / 8) *reinterpret_cast<u32x4*>(&lat[t][tid * 8]) = ldg16(src + tid * 8);
-      continue;
-    }
+    if (ns <= 1) continue;
     const int slice = tid / C4, c = tid % C4;
     float m = kLowest, l = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -514,16 +513,19 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
         v += part[k][tid] * f;
       }
       v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-      *reinterpret_cast<bf16x4*>(&lat[t][tid * 4]) = to_bf16x4(v);
+      put(t, tid, v);
     }
     __syncthreads();
   }
   __syncthreads();
 
   const int t = min(l16, TG - 1);
-  bf16x8 b[KS];
+  bf16x8 b[2][KS];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) b[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[t][ks * 32 + 8 * gq]));
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      b[k][ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[k][t][ks * 32 + 8 * gq]));
   for (int vb = wave; vb < a.d_v / 16; vb += 4) {
     const uint16_t* w = a.w_uv + ((int64_t)h * a.d_v + vb * 16 + l16) * DC;
     f32x4 acc = {};
@@ -531,7 +533,8 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
     for (int ks = 0; ks < KS; ++ks) {
       u32x4 x = {0, 0, 0, 0};
       if (ks * 32 + 8 * gq < DC) x = ldg16(w + ks * 32 + 8 * gq);
-      acc = mfma16(as_bf16x8(x), b[ks], acc);
+      acc = mfma16(as_bf16x8(x), b[0][ks], acc);
+      acc = mfma16(as_bf16x8(x), b[1][ks], acc);
     }
     if (l16 < TG && tok_ns[t] > 0)
       *reinterpret_cast<bf16x4*>(a.out + ((int64_t)(t0 + t) * H + h) * a.d_v + vb * 16 + 4 * gq) = to_bf16x4(acc);
@@ -543,6 +546,12 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
 }  // namespace
 
 void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit) {
+  const int wide = paged_wide_rows(d_c, d_rope);
+  if (wide > 0 && max_rows > 32) {
+    *rows = wide;
+    *unit = 32;
+    return;
+  }
   *rows = max_rows <= 16 ? 16 : 32;
   *unit = 32 * few_waves(d_c);
 }
@@ -553,6 +562,7 @@ hipError_t launch_paged_plan(const PagedAttendArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
+  if (a.rows > 32) return launch_paged_attend_wide(a, s);
 #define X(DC, DR)                                                                                     \
   if (a.d_c == DC && a.d_rope == DR) {                                                                \
     if (a.rows == 16)                                                                                 \

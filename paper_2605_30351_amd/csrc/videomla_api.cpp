@@ -1095,7 +1095,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
     return off;
   };
   L.qcat = take((size_t)rows * qk * 2);
-  L.o_lat = take((size_t)rows * d->d_c * 2);
+  L.o_lat = take((size_t)rows * d->d_c * 4);
   L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
   L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);
   L.zero = take(qk * 2);
@@ -1159,7 +1159,7 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   PagedAttendArgs a{};
   a.q_nope = q_nope; a.q_r = q_r; a.w_uk = w_uk; a.w_uv = w_uv; a.c_kv = c_kv; a.k_r = k_r; a.out = out;
   a.qcat = reinterpret_cast<uint16_t*>(ws + L.qcat);
-  a.o_lat = reinterpret_cast<uint16_t*>(ws + L.o_lat);
+  a.o_lat = reinterpret_cast<float*>(ws + L.o_lat);
   a.o_part = reinterpret_cast<float*>(ws + L.o_part);
   a.ml_part = reinterpret_cast<float*>(ws + L.ml);
   a.zero_row = reinterpret_cast<uint16_t*>(ws + L.zero);

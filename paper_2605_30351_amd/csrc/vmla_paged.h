@@ -6,10 +6,7 @@
 // leaves the tensors: offsets are clamped to the call's token rows, lengths to the table's width, and
 // a table entry outside the pool is a hole.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
-
-#include "vmla_internal.h"
+#include "vmla_device.h"
 
 namespace vmla {
 
@@ -117,6 +114,26 @@ __device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q,
   b = (int32_t)(beg < 0 ? 0 : beg > e ? e : beg);
 }
 
+// The running maximum starts at the lowest finite value, not at -inf: a row that has seen nothing yet
+// (and one that never will) then keeps all its exponentials at exp2(-inf) = 0, with no inf - inf.
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kMasked = -__builtin_huge_valf();
+constexpr float kLazyMaxStep = 8.0f;  // the running max is raised when exceeded by more (log2 units)
+
+// bf16 values with infinities and NaN replaced by zero. In a tile that is masked for some row, a key's
+// probability may be 0 while its latent is not finite, and 0 * NaN would reach the rows that do not see
+// it; a row that does see it has a NaN score, since the latent is part of the key.
+__device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 v) {
+  u32x4 u = as_u32x4(v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = (u[i] & 0x7f80u) == 0x7f80u ? 0u : u[i] & 0xffffu;
+    const uint32_t hi = (u[i] & 0x7f800000u) == 0x7f800000u ? 0u : u[i] & 0xffff0000u;
+    u[i] = lo | hi;
+  }
+  return as_bf16x8(u);
+}
+
 // The plan of one attention call, in the workspace: written by paged_plan_kernel, read by the
 // attention and the output kernels of the same call.
 //   Row blocks: the (token, head) rows of a sequence in blocks of R, sequences in order. A block's keys
@@ -124,13 +141,16 @@ __device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q,
 //   sees nothing keeps one unit: it still writes its rows).
 //   Work: the units of all blocks in order, split evenly over G workgroups; workgroup w takes
 //   [w U / G, (w + 1) U / G). Consecutive units of one block are a segment. A block inside one workgroup
-//   is written as bf16 latents; of a split one each workgroup leaves a partial result, in slot 2 w + 1
-//   for the block's first segment and 2 w for a later one (a workgroup has at most one of each).
+//   is written as its latents; of a split one each workgroup leaves a partial result, in slot 2 w + 1
+//   for the block's first segment and 2 w for a later one (a workgroup has at most one of each). A
+//   workgroup takes its segments last to first: all ranges are equally long, the last segment starts at
+//   a block's first key and the first ends at a block's last, so that the workgroups walk the keys of a
+//   sequence at about the same place at the same time and find tiles in their XCD's L2.
 struct PagedBlock {
   int32_t seq, row0, key0, n_units;
 };
 struct PagedWork {
-  int32_t block, first, n_units, pad;  // first row block, first unit in it, units of the workgroup
+  int32_t block, end, n_units, pad;  // last row block, the end in its units, units of the workgroup
 };
 struct PagedPlan {
   int64_t* head;        // [2]: units U, workgroups G in use
@@ -147,7 +167,7 @@ struct PagedWriteArgs : WriteArgs {
 struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
-  uint16_t* o_lat;     // workspace: [n_tokens * H][d_c] bf16, rows of unsplit blocks
+  float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
   uint16_t* zero_row;  // workspace: a row of zeros, staged in a hole's place
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
@@ -161,8 +181,11 @@ hipError_t launch_paged_plan(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s);
 
-// Rows per block and keys per unit of the attention kernel for at most max_new tokens a sequence.
+// Rows per block and keys per unit of the attention kernel for sequences of at most max_rows rows.
 void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit);
+// The kernel of many rows per block (k_paged_wide.hip): its block, 0 where it is not built, and launch.
+int paged_wide_rows(int d_c, int d_rope);
+hipError_t launch_paged_attend_wide(const PagedAttendArgs& a, hipStream_t s);
 
 constexpr int kCopyPairs = 440;  // page pairs per launch: they travel in the kernel's arguments
 struct PagesCopyArgs {
