@@ -427,8 +427,8 @@ int videomla_dense_attend(const videomla_dims* dims, const videomla_window* win,
  *                  front of the table and first_pos rises by their tokens
  *   block_table    device int32 [n_seqs][max_pages]. An entry outside [0, n_pages) is a hole: its
  *                  tokens are written nowhere and seen by nobody (evicted from the middle, say)
- *   timer          a caller-owned timer, or NULL (kernels "paged_plan", "paged_absorb", "paged_attend",
- *                  "paged_out", "paged_cache_write")
+ *   timer          a caller-owned timer, or NULL (kernels "paged_absorb", "paged_attend", "paged_out",
+ *                  "paged_cache_write")
  * The arrays are read by the kernels: a captured graph replays with the lengths, positions and pages
  * that they hold then. Values out of range are clamped (lengths to what the table can name, offsets to
  * the rows), so that none of them makes a call leave its buffers. Two rows that name the same place of

@@ -16,6 +16,7 @@
 #include <type_traits>
 #include "vmla_device.h"
 #include "vmla_paged.h"
+#include "vmla_paged_plan.h"
 
 namespace vmla {
 namespace {
@@ -40,10 +41,17 @@ template <int DC> struct AbsorbChunk {  // W_UK_h columns staged in LDS per pass
 };
 
 // Args = PagedAttendArgs: the tokens are those of several sequences one after the other (batch 1, Nq =
-// all token rows), each at its sequence's own position.
+// all token rows), each at its sequence's own position; the first workgroup makes the call's plan.
 template <int DC, int DR, class Args>
 __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   constexpr bool PAGED = std::is_same<Args, PagedAttendArgs>::value;
+  if constexpr (PAGED) {
+    if (blockIdx.x == 0) {
+      if (blockIdx.y == 0) paged_plan(a);
+      return;
+    }
+  }
+  const int bx = (int)blockIdx.x - (PAGED ? 1 : 0);
   constexpr int DCP = AbsorbChunk<DC>::DCP;
   constexpr int CW = AbsorbChunk<DC>::CW;  // columns per pass (LDS holds d_nope x CW)
   constexpr int WS = CW + 8;               // LDS row stride (elements)
@@ -59,7 +67,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   const int H = a.n_heads, dn = a.d_nope, Nq = a.geo.q_count;
   const int nks = dn / 16;
 
-  const int n = blockIdx.x * 128 + wave * 32 + l32;
+  const int n = bx * 128 + wave * 32 + l32;
   const bool ok = n < Nq;
   VMLA_STAMP(a, kStampQAbsorb, 0);
   const size_t row = ((size_t)b * Nq + (ok ? n : 0)) * H + h;
@@ -78,7 +86,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   constexpr int NP = DR / 2;
   constexpr bool PAIR_PER_LANE = 64 % NP == 0;
   constexpr int TPI = PAIR_PER_LANE ? 64 / NP : 1, NIT = (32 + TPI - 1) / TPI;
-  const int tok0 = blockIdx.x * 128 + wave * 32;
+  const int tok0 = bx * 128 + wave * 32;
   uint32_t qraw[PAIR_PER_LANE ? NIT : 1];
   RopePair rp{};
   if constexpr (PAIR_PER_LANE) {
@@ -93,13 +101,14 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   // by lanes 0..31 while the loads are in flight (the divisions that split a token index into
   // its position would otherwise be repeated by every lane that rotates one of its pairs)
   __shared__ double qpos[4][3][32];
+  int seq = -1;
+  if constexpr (PAGED) seq = paged_seq_of_lanes(a.pg, min(tok0 + lane, Nq - 1));
   if (lane < 32) {
     TokenPos tp{};
     if constexpr (PAGED) {
-      const int t = min(tok0 + lane, Nq - 1), s = paged_seq_of(a.pg, t);
-      if (s >= 0) {
-        const PagedSeq q = paged_seq(a.pg, s);
-        paged_pos(a.pg, q.first + q.kv - (q.hi - t), tp.f, tp.y, tp.x);
+      if (seq >= 0) {
+        const PagedSeq q = paged_seq(a.pg, seq);
+        paged_pos(a.pg, q.first + q.kv - (q.hi - min(tok0 + lane, Nq - 1)), tp.f, tp.y, tp.x);
       }
     } else {
       tp = rope_pos(a.geo, query_pos(a.geo, min(tok0 + lane, Nq - 1)));
@@ -1209,7 +1218,7 @@ hipError_t launch_q_absorb(const AttendArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s) {
-  const dim3 grid((a.pg.n_tokens + 127) / 128, a.n_heads);
+  const dim3 grid((a.pg.n_tokens + 127) / 128 + 1, a.n_heads);
   const size_t lds = q_absorb_lds_bytes(a.d_c, a.d_rope, a.d_nope);
 #define X(DC, DR)                                                                            \
   if (a.d_c == DC && a.d_rope == DR) {                                                       \

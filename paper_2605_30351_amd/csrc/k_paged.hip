@@ -1,8 +1,8 @@
 // Latent attention of new tokens over a paged cache (Section "Inference-Time Reparameterization", with
 // a sequence's cached tokens in pages instead of a ring).
 //
-//   paged_plan     row blocks, their key ranges and the even split of the work (vmla_paged.h)
-//   q_absorb       as for the ring (k_attend.hip), each token at its sequence's position
+//   q_absorb       as for the ring (k_attend.hip), each token at its sequence's position; and, by one
+//                  workgroup, the plan: row blocks, their key ranges and the even split of the work
 //   paged_attend   S^T = [c_kv | k_r] q_cat^T, masked, online softmax in base 2, O_lat^T += c_kv^T P^T
 //   paged_out      merges the partial results of split row blocks, divides by the sum, applies W_UV_h
 //
@@ -22,6 +22,8 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+typedef __attribute__((address_space(3))) int32_t lds_i32;
+
 // Direct global-to-LDS load of 4 B per lane: lane l's word lands at lds_base + 4 l (see lds_dma16).
 __device__ __forceinline__ void lds_dma4(const int32_t* gptr, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off"
@@ -30,107 +32,18 @@ __device__ __forceinline__ void lds_dma4(const int32_t* gptr, uint32_t lds_base)
                : "memory", "m0");
 }
 
-// ---- plan -----------------------------------------------------------------------------------
-// One workgroup. Sequences, then row blocks, are scanned 1,024 at a time.
-constexpr int kPlanThreads = 1024;
-
-// Exclusive prefix sums of v over the workgroup's threads; total: the sum.
-__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t& total) {
-  __shared__ int64_t wave_sum[kPlanThreads / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  __syncthreads();  // the previous scan's sums are read
-  if (lane == 63) wave_sum[wave] = x;
-  __syncthreads();
-  int64_t base = 0;
-  total = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) base += wave_sum[w];
-    total += wave_sum[w];
-  }
-  return base + x - v;
+// The same of 16 B from a scalar base and a lane offset in bytes. The base has to be settled (no VALU
+// instruction may write it in the five wait states before): callers compute it with scalar arithmetic.
+__device__ __forceinline__ void lds_dma16_row(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(lds_base)
+               : "memory", "m0");
 }
-
-__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PagedAttendArgs a) {
-  __shared__ int32_t first_block[kPagedMaxSeqs + 1];
-  const PagedGeo& g = a.pg;
-  const int tid = threadIdx.x, H = a.n_heads, R = a.rows;
-  int64_t blocks = 0;
-  for (int s0 = 0; s0 < g.n_seqs; s0 += kPlanThreads) {
-    const int s = s0 + tid;
-    int64_t n = 0, total;
-    if (s < g.n_seqs) {
-      const PagedSeq q = paged_seq(g, s);
-      n = ((int64_t)(q.hi - q.lo) * H + R - 1) / R;
-    }
-    const int64_t at = blocks + plan_scan(n, total);
-    // offsets that go down could ask for more blocks than the call's rows make: those are left out
-    if (s < g.n_seqs) first_block[s] = (int32_t)min(at, (int64_t)a.max_blocks);
-    blocks += total;
-  }
-  blocks = min(blocks, (int64_t)a.max_blocks);
-  if (tid == 0) first_block[g.n_seqs] = (int32_t)blocks;
-  __syncthreads();
-  for (int s = tid; s <= g.n_seqs; s += kPlanThreads) a.plan.seq_block[s] = first_block[s];
-  int64_t units = 0;
-  for (int r0 = 0; r0 < blocks; r0 += kPlanThreads) {
-    const int r = r0 + tid;
-    int64_t n = 0, total;
-    if (r < blocks) {
-      int lo = 0, hi = g.n_seqs - 1;  // the last s with first_block[s] <= r
-      while (lo < hi) {
-        const int m = (lo + hi + 1) >> 1;
-        if (first_block[m] <= r) lo = m;
-        else hi = m - 1;
-      }
-      const PagedSeq q = paged_seq(g, lo);
-      const int row0 = (r - first_block[lo]) * R, n_rows = (q.hi - q.lo) * H;
-      const int base = q.kv - (q.hi - q.lo);  // cached index of the sequence's first new token
-      int32_t b, e, b1, e1;
-      paged_seen(g, q, base + row0 / H, b, e);
-      paged_seen(g, q, base + (min(row0 + R, n_rows) - 1) / H, b1, e1);
-      PagedBlock p;
-      p.seq = lo;
-      p.row0 = row0;
-      p.key0 = b & ~31;
-      p.n_units = max(1, (int)(((int64_t)e1 - p.key0 + a.unit - 1) / a.unit));
-      a.plan.block[r] = p;
-      n = p.n_units;
-    }
-    const int64_t at = units + plan_scan(n, total);
-    if (r < blocks) a.plan.first_unit[r] = at;
-    units += total;
-  }
-  if (tid == 0) {
-    a.plan.first_unit[blocks] = units;
-    a.plan.head[0] = units;
-    a.plan.head[1] = min(units, (int64_t)a.n_wg);
-  }
-  __syncthreads();
-  const int64_t G = min(units, (int64_t)a.n_wg);
-  for (int w = tid; w < a.n_wg; w += kPlanThreads) {
-    PagedWork k{};
-    if (w < G) {
-      const int64_t u = floor_div((int64_t)w * units, G), u1 = floor_div((int64_t)(w + 1) * units, G);
-      int lo = 0, hi = (int)blocks - 1;  // the last block with first_unit < u1
-      while (lo < hi) {
-        const int m = (lo + hi + 1) >> 1;
-        if (a.plan.first_unit[m] < u1) lo = m;
-        else hi = m - 1;
-      }
-      k.block = lo;
-      k.end = (int32_t)(u1 - a.plan.first_unit[lo]);
-      k.n_units = (int32_t)(u1 - u);
-    }
-    a.plan.work[w] = k;
-  }
-  // the row that is staged in place of a hole
-  for (int i = tid; i < a.dqk_pad; i += kPlanThreads) a.zero_row[i] = 0;
+// Waits until at most N vector-memory operations of the wave are outstanding; later LDS reads stay behind.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
 // ---- attention of few rows -------------------------------------------------------------------
@@ -150,8 +63,15 @@ struct FewCfg {
   static constexpr int NDMA = 32 * CPR / 64;             // 1 KB loads per tile
   static constexpr int NW = few_waves(DC);
   static constexpr int ROWS = 16 * QB;
+  static constexpr int QP = QB % 2 ? 1 : 2;              // 16-row blocks merged at a time
   static constexpr int UNIT = 32 * NW;
   static constexpr int RS = DC + 4;                      // row stride of the merged latents (floats)
+  // Tile layout. d_c = 512: c_kv rows of 1 KB, so that a load is one row from a scalar base, then the k_r
+  // rows. Otherwise rows [c_kv | k_r | pad].
+  static constexpr bool SPLIT = DC == 512;
+  static constexpr int STRIDE = SPLIT ? DC : DQKP;
+  // The queries are in LDS where with the accumulators they would fill the registers.
+  static constexpr bool QLDS = QB * (KS + DV) * 4 > 190;
   // Chunk position of logical chunk c in row r. CPR is 4 or 12 mod 16, so the rows r .. r + 3 of one
   // chunk fall on different groups of four 4-bank groups; the XOR separates the rows 4 apart, by bit 1
   // first, since the transpose reads take two adjacent chunks of rows 4 j .. 4 j + 3 and the next four.
@@ -159,9 +79,12 @@ struct FewCfg {
     const int q = (r >> 2) & 3;
     return ((q & 1) << 1) | (q >> 1);
   }
+  // SPLIT: rows of 64 chunks start on the same banks, so the XOR separates all 16 rows, and the rows
+  // 0 .. 7 and 8 .. 15 of the transpose reads by pairs of chunks.
+  __device__ static constexpr int swz16(int r) { return ((r << 1) & 15) | ((r >> 3) & 1); }
   static_assert(CPR % 16 == 4 || CPR % 16 == 12, "bank spread of the tile rows");
   static_assert(DC % 16 == 0 && 16 * CPR % 64 == 0 && NDMA + 1 < 64, "tile shape");
-  static_assert(ROWS * RS * 4 <= 2 * TILE * 2, "a wave's results fit its tile buffers");
+  static_assert(16 * QP * RS * 4 <= 2 * TILE * 2, "a wave's results fit its tile buffers");
 };
 
 template <int DC, int DR, int QB>
@@ -169,70 +92,83 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
   using C = FewCfg<DC, DR, QB>;
   constexpr int NW = C::NW;
   __shared__ __attribute__((aligned(16))) uint16_t tiles[NW][2][C::TILE];
+  __shared__ __attribute__((aligned(16))) uint16_t qs[C::QLDS ? C::ROWS * C::DQKP : 8];
   __shared__ int32_t ids[NW][2][64];
-  __shared__ float red_m[NW][C::ROWS], red_l[NW][C::ROWS];
+  __shared__ float red_m[NW][16 * C::QP], red_l[NW][16 * C::QP];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int gq = lane >> 4, l16 = lane & 15;
   const PagedGeo& g = a.pg;
   const int H = a.n_heads;
-  const PagedWork wk = a.plan.work[blockIdx.x];
-  int left = __builtin_amdgcn_readfirstlane(wk.n_units);
-  int blk = __builtin_amdgcn_readfirstlane(wk.block), end = __builtin_amdgcn_readfirstlane(wk.end);
+  const PagedWork wk = paged_read<true>(a.plan.work, blockIdx.x);
+  int left = wk.n, blk = wk.block, end = wk.end;
 
   // Load j of a tile fills the chunk slots 64 j .. 64 j + 63: of this lane's chunk, in bits 0..15 the
   // offset in its row's c_kv, or (bit 31) k_r (the pad reads k_r again, against zeros in q_cat), in bits
   // 16..19 the row modulo 16. Half a tile is a whole number of loads, and the other half repeats it.
-  uint32_t d_at[C::NDMA / 2];
+  // (SPLIT: of the two loads of k_r, from load 32 on.)
+  constexpr int NAT = C::SPLIT ? 1 : C::NDMA / 2;
+  uint32_t d_at[NAT];
+  if constexpr (C::SPLIT) {
+    const int r = lane >> 2;
+    d_at[0] = 0x80000000u | (uint32_t)r << 16 | (((lane & 3) ^ C::swz(r)) * 8);
+  } else {
 #pragma unroll
-  for (int j = 0; j < C::NDMA / 2; ++j) {
-    const int slot = j * 64 + lane, r = slot / C::CPR, c = (slot % C::CPR) ^ C::swz(r);
-    d_at[j] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : 0x80000000u | (c < (DC + DR) / 8 ? c * 8 - DC : 0));
+    for (int j = 0; j < NAT; ++j) {
+      const int slot = j * 64 + lane, r = slot / C::CPR, c = (slot % C::CPR) ^ C::swz(r);
+      d_at[j] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : 0x80000000u | (c < (DC + DR) / 8 ? c * 8 - DC : 0));
+    }
   }
 
   while (left > 0) {
-    const PagedBlock pb = a.plan.block[blk];
-    const int seq = __builtin_amdgcn_readfirstlane(pb.seq), row0 = __builtin_amdgcn_readfirstlane(pb.row0);
-    const int n_units = __builtin_amdgcn_readfirstlane(pb.n_units);
-    if (end == 0) end = n_units;  // a segment before the workgroup's last ends with its block
-    const int take = min(left, end), u0 = end - take;
-    const int key0 = __builtin_amdgcn_readfirstlane(pb.key0) + u0 * C::UNIT + wave * 32;  // this wave's first
-    const PagedSeq q = paged_seq<true>(g, seq);
-    const int n_rows = (q.hi - q.lo) * H, base = q.kv - (q.hi - q.lo);
-    const int32_t* table = g.table + (int64_t)seq * g.max_pages;
+    const PagedBlock pb = paged_read<true>(a.plan.block, blk);
+    if (end < 0) end = pb.n_units + a.cost;  // a block before the workgroup's last is taken to its end
+    const int len = min(left, end), u1 = end - a.cost, u0 = max(u1 - len, 0), take = u1 - u0;
+    left -= len;
+    end = -1;
+    --blk;
+    if (take <= 0) continue;
+    const int key0 = pb.key0 + u0 * C::UNIT + wave * 32;  // this wave's first
+    const int row0 = pb.row0, n_rows = pb.n_rows;
+    const int32_t* table = g.table + (int64_t)pb.seq * g.max_pages;
+
+    // page ids of tile t's keys, one per lane, into slot t & 1 (a key outside the sequence reads the
+    // nearest entry of the table, and is no row below)
+    auto load_ids = [&](int t) {
+      const int key = min(key0 + t * C::UNIT + (lane & 31), g.max_kv - 1);
+      lds_dma4(table + page_of(g, key), __builtin_amdgcn_readfirstlane(lds_addr(&ids[wave][t & 1][0])));
+    };
+    load_ids(0);
 
     // this lane's rows and what they see
-    bf16x8 qv[QB][C::KS];
+    bf16x8 qv[C::QLDS ? 1 : QB][C::KS];
     int see_b[QB], see_e[QB];
-    int b_max = 0, e_min = 0x7fffffff;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int r = row0 + 16 * qb + l16;
       see_b[qb] = 0;
       see_e[qb] = 0x7fffffff;
-      if (r < n_rows) {
-        paged_seen(g, q, base + r / H, see_b[qb], see_e[qb]);
-        b_max = max(b_max, see_b[qb]);
-        e_min = min(e_min, see_e[qb]);
-      }
-      const uint16_t* src = a.qcat + ((int64_t)q.lo * H + (r < n_rows ? r : row0)) * a.dqk_pad;
+      if (r < n_rows) paged_row_sees(g, pb, H, 16 * qb + l16, see_b[qb], see_e[qb]);
+      if constexpr (!C::QLDS) {
+        const uint16_t* src = a.qcat + ((int64_t)pb.lo * H + (r < n_rows ? r : row0)) * C::DQKP + 8 * gq;
 #pragma unroll
-      for (int ks = 0; ks < C::KS; ++ks) {
-        const int c = ks * 32 + 8 * gq;
-        u32x4 v = {0, 0, 0, 0};
-        if (r < n_rows && c < a.dqk_pad) v = ldg16(src + c);
-        qv[qb][ks] = as_bf16x8(v);
+        for (int ks = 0; ks < C::KS; ++ks) {
+          u32x4 v = ldg16(src + ks * 32);
+          if (r >= n_rows) v = u32x4{0, 0, 0, 0};
+          qv[qb][ks] = as_bf16x8(v);
+        }
       }
     }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-      b_max = max(b_max, __shfl_xor(b_max, d));
-      e_min = min(e_min, __shfl_xor(e_min, d));
+    if constexpr (C::QLDS) {  // laid out as the tile's rows, so that the reads are as free of conflicts
+      for (int i = threadIdx.x; i < C::ROWS * C::CPR; i += NW * 64) {
+        const int r = i / C::CPR, c = i % C::CPR;
+        u32x4 v = ldg16(a.qcat + ((int64_t)pb.lo * H + row0 + (row0 + r < n_rows ? r : 0)) * C::DQKP + c * 8);
+        if (row0 + r >= n_rows) v = u32x4{0, 0, 0, 0};
+        *reinterpret_cast<u32x4*>(&qs[r * C::DQKP + (c ^ C::swz(r)) * 8]) = v;
+      }
+      __syncthreads();
     }
-    b_max = __builtin_amdgcn_readfirstlane(b_max);
-    e_min = __builtin_amdgcn_readfirstlane(e_min);
-
     f32x4 o[QB][C::DV];
     float m_run[QB], l_run[QB];
 #pragma unroll
@@ -243,68 +179,102 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       for (int d = 0; d < C::DV; ++d) o[qb][d] = f32x4{};
     }
 
-    // page ids of tile t's keys, one per lane, into slot t & 1 (a key outside the sequence reads the
-    // nearest entry of the table, and is no row below)
-    auto load_ids = [&](int t) {
-      const int key = min(max(key0 + t * C::UNIT + (lane & 31), 0), g.max_kv - 1);
-      lds_dma4(table + page_of(g, key), __builtin_amdgcn_readfirstlane(lds_addr(&ids[wave][t & 1][0])));
-    };
     auto row_of = [&](int t) {  // this lane's key's pool row, -1: none
       const int key = key0 + t * C::UNIT + (lane & 31);
-      const int32_t page = *(volatile int32_t*)&ids[wave][t & 1][lane];
-      if (key >= q.kv || page < 0 || page >= g.n_pages) return -1;
+      // (through an LDS pointer: a generic one would wait for every load in flight)
+      const int32_t page = *(const volatile lds_i32*)(&ids[wave][t & 1][lane]);
+      if (key >= pb.kv || page < 0 || page >= g.n_pages) return -1;
       return page * g.page_tokens + key - page_of(g, key) * g.page_tokens;
     };
     auto load_tile = [&](int t, int row) {
-      const uint32_t lds = lds_addr(&tiles[wave][t & 1][0]);
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(&tiles[wave][t & 1][0]));
+      if constexpr (C::SPLIT) {
 #pragma unroll
-      for (int j = 0; j < C::NDMA; ++j) {
-        const uint32_t at = d_at[j % (C::NDMA / 2)];
-        const int32_t r = __shfl(row, (int)(at >> 16 & 15) + (j < C::NDMA / 2 ? 0 : 16));
+        for (int j = 0; j < 32; ++j) {
+          const int32_t r = __builtin_amdgcn_readlane(row, j);
+          lds_dma16_row(r < 0 ? a.zero_row : a.c_kv + (int64_t)r * DC, (lane ^ C::swz16(j)) * 16, lds + 1024u * j);
+        }
+      }
+#pragma unroll
+      for (int j = C::SPLIT ? 32 : 0; j < C::NDMA; ++j) {
+        const int half = C::SPLIT ? j - 32 : j / NAT;
+        uint32_t at = d_at[j % NAT];
+        // recomputed from one register a load: kept across the loop, the addresses' parts would fill the file
+        if constexpr (QB * DC >= 256) asm volatile("" : "+v"(at));
+        const int32_t r = __shfl(row, (int)(at >> 16 & 15) + 16 * half);
         const bool kr = (int32_t)at < 0;
         const uint16_t* p = kr ? a.k_r : a.c_kv;
         p += (int64_t)r * (kr ? DR : DC) + (at & 0xffffu);
-        lds_dma16(r < 0 ? a.zero_row : p, __builtin_amdgcn_readfirstlane(lds + 1024u * j));
+        lds_dma16(r < 0 ? a.zero_row : p, lds + 1024u * j);
       }
     };
 
-    // the tile rows' K operand of step ks (lane: row l16 + 16 kb, chunk 4 ks + gq) and the transpose
-    // reads' rows 4 gq + .. (lane: row 4 gq + l16 / 4 (+ 16), columns 4 (l16 % 4) + 16 d)
-    const int k_sw = C::swz(l16), v_sw = C::swz(4 * gq);
-    const int v_row = 4 * gq + (l16 >> 2), v_col = l16 & 3;
+    // The K operand of step ks (lane: row l16 + 16 kb, chunk 4 ks + gq) and the transpose reads' rows (lane:
+    // row 4 gq + l16 / 4 (+ 16), columns 4 (l16 % 4) + 16 d). The XORs stay below 4 (SPLIT: 16) chunks, so
+    // that a few bases and immediate offsets reach every step.
+    const int v_row = 4 * gq + (l16 >> 2), v_ch = (l16 >> 1) & 1;
+    constexpr int NKB = C::SPLIT ? 5 : 1, NVB = C::SPLIT ? 8 : 2;
+    int k_base[NKB], v_base[NVB];
+    if constexpr (C::SPLIT) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k_base[i] = l16 * DC + (((4 * i + gq) ^ C::swz16(l16)) << 3);
+      k_base[4] = 32 * DC + l16 * DR + ((gq ^ C::swz(l16)) << 3);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v_base[i] = v_row * DC + (((2 * i + v_ch) ^ C::swz16(v_row)) << 3) + (l16 & 1) * 4;
+    } else {
+      k_base[0] = l16 * C::DQKP + ((gq ^ C::swz(l16)) << 3);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        v_base[i] = v_row * C::DQKP + (((2 * i + v_ch) ^ C::swz(v_row)) << 3) + (l16 & 1) * 4;
+    }
+    auto k_at = [&](int kb, int ks) {
+      if constexpr (C::SPLIT)
+        return ks < DC / 32 ? k_base[ks & 3] + kb * 16 * DC + (ks >> 2) * 128 : k_base[4] + kb * 16 * DR;
+      else return k_base[0] + kb * 16 * C::DQKP + ks * 32;
+    };
+    auto v_at = [&](int d) {
+      if constexpr (C::SPLIT) return v_base[d & 7] + (d >> 3) * 128;
+      else return v_base[d & 1] + (d >> 1) * 32;
+    };
+    auto q_at = [&](int qb, int ks) {
+      if constexpr (C::QLDS)
+        return as_bf16x8(*reinterpret_cast<const u32x4*>(
+            &qs[(16 * qb + l16) * C::DQKP + ((gq ^ C::swz(l16)) << 3) + ks * 32]));
+      else return qv[qb][ks];
+    };
 
-    load_ids(0);
-    wait_vmcnt<0>();
+    wait_loads<0>();
     int row = row_of(0);
     load_ids(1);
     load_tile(0, row);
     for (int t = 0; t < take; ++t) {
       const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);  // keys of tile t that exist
       if (t + 1 < take) {
-        wait_vmcnt<C::NDMA>();  // the ids of tile t + 1
+        wait_loads<C::NDMA>();  // the ids of tile t + 1
         row = row_of(t + 1);
         load_ids(t + 2);
         load_tile(t + 1, row);
-        wait_vmcnt<C::NDMA + 1>();  // tile t
+        wait_loads<C::NDMA + 1>();  // tile t
       } else {
-        wait_vmcnt<0>();
+        wait_loads<0>();
       }
       if (there == 0) continue;
       const int k0 = key0 + t * C::UNIT;
       const uint16_t* tile = tiles[wave][t & 1];
-      const bool masked = there != 0xffffffffu || k0 < b_max || k0 + 32 > e_min;
+      const bool masked = there != 0xffffffffu || k0 < pb.all_b || k0 + 32 > pb.all_e;
 
       f32x4 s[QB][2];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{};
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{};
+      for (int ks = 0; ks < C::KS; ++ks) {
+        const bf16x8 k0v = as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[k_at(0, ks)]));
+        const bf16x8 k1v = as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[k_at(1, ks)]));
 #pragma unroll
-        for (int ks = 0; ks < C::KS; ++ks) {
-          const bf16x8 k = as_bf16x8(*reinterpret_cast<const u32x4*>(
-              &tile[(16 * kb + l16) * C::DQKP + ((4 * ks + gq) ^ k_sw) * 8]));
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) s[qb][kb] = mfma16(k, qv[qb][ks], s[qb][kb]);
+        for (int qb = 0; qb < QB; ++qb) {
+          const bf16x8 qk = q_at(qb, ks);
+          s[qb][0] = mfma16(k0v, qk, s[qb][0]);
+          s[qb][1] = mfma16(k1v, qk, s[qb][1]);
         }
       }
       if (masked) {
@@ -358,65 +328,69 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
                                 __builtin_bit_cast(uint32_t, h[2]), __builtin_bit_cast(uint32_t, h[3])});
       }
       // keys 4 gq + 0 .. 3 and 16 + 4 gq + 0 .. 3 in k-order, for both operands
-      const uint16_t* v0 = tile + v_row * C::DQKP + (v_col & 1) * 4;
+      auto pv = [&](auto clear) {
 #pragma unroll
-      for (int d = 0; d < C::DV; ++d) {
-        const int ch = ((2 * d + (v_col >> 1)) ^ v_sw) * 8;
-        const i16x4 lo = lds_read_tr(v0 + ch), hi = lds_read_tr(v0 + 16 * C::DQKP + ch);
-        bf16x8 v = join_bf16x8(lo, hi);
-        if (masked) v = finite_or_zero(v);
+        for (int d = 0; d < C::DV; ++d) {
+          const uint16_t* v0 = tile + v_at(d);
+          const i16x4 lo = lds_read_tr(v0), hi = lds_read_tr(v0 + 16 * C::STRIDE);
+          bf16x8 v = join_bf16x8(lo, hi);
+          if constexpr (decltype(clear)::value) v = finite_or_zero(v);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) o[qb][d] = mfma16(v, p[qb], o[qb][d]);
-      }
+          for (int qb = 0; qb < QB; ++qb) o[qb][d] = mfma16(v, p[qb], o[qb][d]);
+        }
+      };
+      if (masked) pv(std::true_type{});
+      else pv(std::false_type{});
     }
 
-    // ---- the waves' results, merged in wave order ----
-    float* res = reinterpret_cast<float*>(&tiles[wave][0][0]);  // [ROWS][RS]: this wave's own buffers
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      float l = l_run[qb];
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      if (gq == 0) {
-        red_m[wave][16 * qb + l16] = m_run[qb];
-        red_l[wave][16 * qb + l16] = l;
-      }
-#pragma unroll
-      for (int d = 0; d < C::DV; ++d)
-        *reinterpret_cast<f32x4*>(&res[(16 * qb + l16) * C::RS + 16 * d + 4 * gq]) = o[qb][d];
-    }
-    __syncthreads();
-    const bool whole = take == n_units;
+    // ---- the waves' results, merged in wave order, 16 QP rows at a time ----
+    float* res = reinterpret_cast<float*>(&tiles[wave][0][0]);  // [16 QP][RS]: this wave's own buffers
+    const bool whole = take == pb.n_units;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (u0 == 0);
-    for (int i = threadIdx.x; i < C::ROWS * (DC / 4); i += NW * 64) {
-      const int r = i / (DC / 4), c = i % (DC / 4) * 4;
-      if (row0 + r >= n_rows) break;
-      float m = kLowest, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][r]);
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int q0 = 0; q0 < QB; q0 += C::QP) {
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float f = fast_exp2(red_m[w][r] - m);
-        l += f * red_l[w][r];
-        v += f * *reinterpret_cast<const f32x4*>(
-                     reinterpret_cast<const float*>(&tiles[w][0][0]) + r * C::RS + c);
+      for (int qp = 0; qp < C::QP; ++qp) {
+        const int qb = q0 + qp;
+        float l = l_run[qb];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (gq == 0) {
+          red_m[wave][16 * qp + l16] = m_run[qb];
+          red_l[wave][16 * qp + l16] = l;
+        }
+#pragma unroll
+        for (int d = 0; d < C::DV; ++d)
+          *reinterpret_cast<f32x4*>(&res[(16 * qp + l16) * C::RS + 16 * d + 4 * gq]) = o[qb][d];
       }
-      if (whole) {
-        v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-        *reinterpret_cast<f32x4*>(a.o_lat + ((int64_t)q.lo * H + row0 + r) * DC + c) = v;
-      } else {
-        *reinterpret_cast<f32x4*>(a.o_part + (slot * C::ROWS + r) * DC + c) = v;
-        if (c == 0) {
-          a.ml_part[(slot * C::ROWS + r) * 2] = m;
-          a.ml_part[(slot * C::ROWS + r) * 2 + 1] = l;
+      __syncthreads();
+      for (int i = threadIdx.x; i < 16 * C::QP * (DC / 4); i += NW * 64) {
+        const int rr = i / (DC / 4), r = 16 * q0 + rr, c = i % (DC / 4) * 4;
+        if (row0 + r >= n_rows) break;
+        float m = kLowest, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][rr]);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const float f = fast_exp2(red_m[w][rr] - m);
+          l += f * red_l[w][rr];
+          v += f * *reinterpret_cast<const f32x4*>(
+                       reinterpret_cast<const float*>(&tiles[w][0][0]) + rr * C::RS + c);
+        }
+        if (whole) {
+          v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
+          *reinterpret_cast<f32x4*>(a.o_lat + ((int64_t)pb.lo * H + row0 + r) * DC + c) = v;
+        } else {
+          *reinterpret_cast<f32x4*>(a.o_part + (slot * C::ROWS + r) * DC + c) = v;
+          if (c == 0) {
+            a.ml_part[(slot * C::ROWS + r) * 2] = m;
+            a.ml_part[(slot * C::ROWS + r) * 2 + 1] = l;
+          }
         }
       }
+      __syncthreads();  // the buffers are free for the next rows or segment
     }
-    __syncthreads();  // the buffers are free for the next segment
-    left -= take;
-    end = 0;
-    --blk;
   }
 }
 
@@ -425,34 +399,86 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
 // row block was split, then out^T[v][token] = W_UV_h[v][:] . o_lat[token][:]. The latents go into the
 // product as two bf16 terms (16 bits of fraction): one alone adds a rounding as large as the output's
 // own, 2^-8 of the value, for a product that costs next to nothing here.
+// TG = 1 (few tokens: single-token steps, whose rows are split the most): the splits are read by slices
+// of the workgroup side by side, each with its own running maximum. More tokens: the coefficient of
+// every (token, split) goes into a table, and a thread sums its chunks, four in flight per split.
+constexpr int kOutSplits = 8;  // splits the table holds; tokens of more are merged one split after the other
+
 template <int DC, int TG>
-__global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a) {
+__global__ __launch_bounds__(256, DC <= 256 ? 3 : 2) void paged_out_kernel(const PagedAttendArgs a) {
   constexpr int LS = (DC > 32 ? DC : 32) + 8;  // LDS row stride (elements)
   constexpr int KS = (DC + 31) / 32;
   constexpr int C4 = DC / 4;                   // 16-byte chunks of a partial row
-  constexpr int SL = 256 / C4 < 16 ? 256 / C4 : 16;  // splits read side by side
+  constexpr int SL = TG > 1 ? 1 : 256 / C4 < 16 ? 256 / C4 : 16;  // slices of splits
+  constexpr int NB = (TG + 15) / 16;           // blocks of 16 tokens
   __shared__ __attribute__((aligned(16))) uint16_t lat[2][TG][LS];  // o_lat's first and second term
   __shared__ f32x4 part[SL][C4];
   __shared__ float part_m[SL], part_l[SL];
-  __shared__ int32_t tok_row[TG], tok_w0[TG], tok_ns[TG];  // (ns 0: no token of a sequence)
+  __shared__ float coef[TG > 1 ? TG : 1][kOutSplits];
+  __shared__ int32_t tok_row[TG], tok_w0[TG], tok_ns[TG], most_s;  // (ns 0: no token of a sequence)
   const PagedGeo& g = a.pg;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, l16 = lane & 15;
   const int H = a.n_heads, h = blockIdx.y, t0 = blockIdx.x * TG;
 
-  if (tid < TG) {
-    const int t = t0 + tid, s = t < g.n_tokens ? paged_seq_of(g, t) : -1;
+  // the weights of the wave's first output blocks, on their way while the latents are merged
+  const int n_vb = a.d_v / 16;
+  auto weight = [&](int vb, int ks) {
+    u32x4 x = {0, 0, 0, 0};
+    if (ks * 32 + 8 * gq < DC) x = ldg16(a.w_uv + ((int64_t)h * a.d_v + vb * 16 + l16) * DC + ks * 32 + 8 * gq);
+    return as_bf16x8(x);
+  };
+  constexpr int AHEAD = DC > 256 ? 1 : 2;
+  bf16x8 wv[AHEAD][KS];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) wv[i][ks] = weight(min(wave * AHEAD + i, n_vb - 1), ks);
+
+  // partial row of split k of a token (its first partial has the first key: slot 2 w + 1)
+  auto part_row = [&](int w0, int k, int row) { return (2 * (int64_t)(w0 + k) + (k == 0)) * a.rows + row; };
+  if (wave == 0) {
+    const int t = t0 + min(lane, TG - 1);
+    const int s0 = paged_seq_of_lanes(g, t), s = t < g.n_tokens ? s0 : -1;
     const int r = s >= 0 ? (t - max(g.cu[s], 0)) * H + h : 0;
     const int blk = s >= 0 ? a.plan.seq_block[s] + r / a.rows : 0;
     const bool known = s >= 0 && blk < a.plan.seq_block[g.n_seqs];  // (else offsets that go down)
-    tok_ns[tid] = 0;
+    int ns = 0, w0 = 0;
     if (known) {
       const int64_t U = a.plan.head[0], G = a.plan.head[1];
-      const int w0 = (int)floor_div((a.plan.first_unit[blk] + 1) * G - 1, U);
-      tok_row[tid] = r % a.rows;
-      tok_w0[tid] = w0;
-      tok_ns[tid] = (int)floor_div(a.plan.first_unit[blk + 1] * G - 1, U) - w0 + 1;
+      w0 = (int)floor_div((a.plan.first[blk] + a.cost + 1) * G - 1, U);
+      ns = (int)floor_div(a.plan.first[blk + 1] * G - 1, U) - w0 + 1;
     }
+    int most = ns;
+    if constexpr (TG > 1) {
+      const int row = r % a.rows;
+      if (ns > 1 && ns <= kOutSplits) {
+        f32x2 ml[kOutSplits];
+#pragma unroll
+        for (int k = 0; k < kOutSplits; ++k)
+          ml[k] = *reinterpret_cast<const f32x2*>(a.ml_part + part_row(w0, min(k, ns - 1), row) * 2);
+        float m = kLowest, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < kOutSplits; ++k) m = fmaxf(m, ml[k][0]);
+#pragma unroll
+        for (int k = 0; k < kOutSplits; ++k) l += k < ns ? fast_exp2(ml[k][0] - m) * ml[k][1] : 0.f;
+        const float il = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing: zeros)
+        if (lane < TG)
+#pragma unroll
+          for (int k = 0; k < kOutSplits; ++k) coef[lane][k] = k < ns ? fast_exp2(ml[k][0] - m) * il : 0.f;
+      } else if (lane < TG) {
+#pragma unroll
+        for (int k = 0; k < kOutSplits; ++k) coef[lane][k] = k == 0 ? 1.f : 0.f;
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+    }
+    if (lane < TG) {
+      tok_ns[lane] = ns;
+      tok_row[lane] = r % a.rows;
+      tok_w0[lane] = w0;
+    }
+    if (lane == 0) most_s = most;
   }
   if constexpr (DC < 32) {
     for (int i = tid; i < 2 * TG * LS; i += 256) (&lat[0][0][0])[i] = 0;
@@ -464,80 +490,138 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
     *reinterpret_cast<bf16x4*>(&lat[0][t][c4 * 4]) = hi;
     *reinterpret_cast<bf16x4*>(&lat[1][t][c4 * 4]) = to_bf16x4(rest);
   };
-
-  // tokens of unsplit blocks: every load issued before the first is used
-  constexpr int PER = (TG * C4 + 255) / 256;
-  f32x4 whole[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = tid + 256 * i, t = e / C4;
-    if (e < TG * C4 && tok_ns[t] == 1)
-      whole[i] = *reinterpret_cast<const f32x4*>(a.o_lat + ((int64_t)(t0 + t) * H + h) * DC + e % C4 * 4);
-  }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = tid + 256 * i, t = e / C4;
-    if (e < TG * C4 && tok_ns[t] == 1) put(t, e % C4, whole[i]);
-  }
-  for (int t = 0; t < TG; ++t) {
+  // the online merge of chunk c of token t's partial results k0, k0 + SL, ..
+  auto merge = [&](int t, int c, int k0, float& m, float& l, f32x4& v) {
     const int ns = tok_ns[t], w0 = tok_w0[t];
-    if (ns <= 1) continue;
-    const int slice = tid / C4, c = tid % C4;
-    float m = kLowest, l = 0.f;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (slice < SL) {
-      for (int k = slice; k < ns; k += SL) {
-        const int64_t row = (2 * (int64_t)(w0 + k) + (k == 0)) * a.rows + tok_row[t];
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.ml_part + row * 2);
-        const f32x4 x = *reinterpret_cast<const f32x4*>(a.o_part + row * DC + c * 4);
-        const float m1 = fmaxf(m, ml[0]), f0 = fast_exp2(m - m1), f1 = fast_exp2(ml[0] - m1);
-        l = l * f0 + ml[1] * f1;
-        v = v * f0 + x * f1;
-        m = m1;
+    m = kLowest;
+    l = 0.f;
+    v = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = k0; k < ns; k += 4 * SL) {
+      f32x2 ml[4];
+      f32x4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int kk = k + j * SL < ns ? k + j * SL : k;  // (past the last: read again, weighed by zero)
+        const int64_t row = part_row(w0, kk, tok_row[t]);
+        ml[j] = *reinterpret_cast<const f32x2*>(a.ml_part + row * 2);
+        x[j] = *reinterpret_cast<const f32x4*>(a.o_part + row * DC + c * 4);
       }
-      part[slice][c] = v;
-      if (c == 0) {
-        part_m[slice] = m;
-        part_l[slice] = l;
+      float m1 = m;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m1 = fmaxf(m1, ml[j][0]);
+      const float f = fast_exp2(m - m1);
+      l *= f;
+      v *= f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (k + j * SL < ns) {
+          const float fj = fast_exp2(ml[j][0] - m1);
+          l += fj * ml[j][1];
+          v += fj * x[j];
+        }
+      }
+      m = m1;
+    }
+  };
+  const int most = most_s;
+  if constexpr (TG == 1) {
+    if (most == 0) return;
+    if (most == 1) {
+      if (tid < C4) put(0, tid, *reinterpret_cast<const f32x4*>(a.o_lat + ((int64_t)t0 * H + h) * DC + tid * 4));
+    } else {
+      const int slice = tid / C4, c = tid % C4;
+      if (slice < SL) {
+        float m, l;
+        f32x4 v;
+        merge(0, c, slice, m, l, v);
+        part[slice][c] = v;
+        if (c == 0) {
+          part_m[slice] = m;
+          part_l[slice] = l;
+        }
+      }
+      __syncthreads();
+      if (tid < C4) {
+        float m = kLowest, l = 0.f;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < SL; ++k) m = fmaxf(m, part_m[k]);
+        for (int k = 0; k < SL; ++k) {
+          const float f = fast_exp2(part_m[k] - m);
+          l += part_l[k] * f;
+          v += part[k][tid] * f;
+        }
+        put(0, tid, v * (l == 0.f ? 0.f : 1.f / l));
       }
     }
-    __syncthreads();
-    if (tid < C4) {
-      m = kLowest;
-      l = 0.f;
-      v = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int k = 0; k < SL; ++k) m = fmaxf(m, part_m[k]);
-      for (int k = 0; k < SL; ++k) {
-        const float f = fast_exp2(part_m[k] - m);
-        l += part_l[k] * f;
-        v += part[k][tid] * f;
+  } else {
+    // chunk e = (token, 4 columns); a token of no sequence reads row 0 and is not stored
+    constexpr int N = (TG * C4 + 255) / 256, IN = N < 4 ? N : 4;
+    auto source = [&](int e, int k) {
+      const int t = min(e / C4, TG - 1), ns = tok_ns[t];
+      const float* p = ns <= 1 ? a.o_lat + ((int64_t)(ns == 0 ? 0 : t0 + t) * H + h) * DC
+                               : a.o_part + part_row(tok_w0[t], min(k, ns - 1), tok_row[t]) * DC;
+      return reinterpret_cast<const f32x4*>(p + e % C4 * 4);
+    };
+#pragma unroll 1
+    for (int i0 = 0; i0 < N; i0 += IN) {
+      f32x4 v[IN];
+#pragma unroll
+      for (int i = 0; i < IN; ++i) v[i] = *source(tid + 256 * (i0 + i), 0);
+      if (most > 1) {
+#pragma unroll
+        for (int i = 0; i < IN; ++i) v[i] *= coef[min((tid + 256 * (i0 + i)) / C4, TG - 1)][0];
+        for (int k = 1; k < min(most, kOutSplits); ++k) {
+          f32x4 x[IN];
+#pragma unroll
+          for (int i = 0; i < IN; ++i) x[i] = *source(tid + 256 * (i0 + i), k);
+#pragma unroll
+          for (int i = 0; i < IN; ++i) {
+            const float f = coef[min((tid + 256 * (i0 + i)) / C4, TG - 1)][k];
+            if (f != 0.f) v[i] += f * x[i];
+          }
+        }
       }
-      v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-      put(t, tid, v);
+#pragma unroll
+      for (int i = 0; i < IN; ++i) {
+        const int e = tid + 256 * (i0 + i), t = e / C4;
+        if (e >= TG * C4) continue;
+        if (tok_ns[t] > kOutSplits) {
+          float m, l;
+          merge(t, e % C4, 0, m, l, v[i]);
+          v[i] *= l == 0.f ? 0.f : 1.f / l;
+        }
+        put(t, e % C4, v[i]);
+      }
     }
-    __syncthreads();
   }
   __syncthreads();
 
-  const int t = min(l16, TG - 1);
-  bf16x8 b[2][KS];
+  for (int vb = wave * AHEAD; vb < n_vb; vb += 4 * AHEAD) {
+    if (vb != wave * AHEAD) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+      for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      b[k][ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[k][t][ks * 32 + 8 * gq]));
-  for (int vb = wave; vb < a.d_v / 16; vb += 4) {
-    const uint16_t* w = a.w_uv + ((int64_t)h * a.d_v + vb * 16 + l16) * DC;
-    f32x4 acc = {};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      u32x4 x = {0, 0, 0, 0};
-      if (ks * 32 + 8 * gq < DC) x = ldg16(w + ks * 32 + 8 * gq);
-      acc = mfma16(as_bf16x8(x), b[0][ks], acc);
-      acc = mfma16(as_bf16x8(x), b[1][ks], acc);
+        for (int ks = 0; ks < KS; ++ks) wv[i][ks] = weight(min(vb + i, n_vb - 1), ks);
     }
-    if (l16 < TG && tok_ns[t] > 0)
-      *reinterpret_cast<bf16x4*>(a.out + ((int64_t)(t0 + t) * H + h) * a.d_v + vb * 16 + 4 * gq) = to_bf16x4(acc);
+#pragma unroll 1
+    for (int nb = 0; nb < NB; ++nb) {
+      const int t = min(16 * nb + l16, TG - 1);
+      f32x4 acc[AHEAD] = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bf16x8 b = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[k][t][ks * 32 + 8 * gq]));
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) acc[i] = mfma16(wv[i][ks], b, acc[i]);
+        }
+      if (16 * nb + l16 < TG && tok_ns[t] > 0) {
+        uint16_t* dst = a.out + ((int64_t)(t0 + t) * H + h) * a.d_v + vb * 16 + 4 * gq;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (vb + i < n_vb) *reinterpret_cast<bf16x4*>(dst + i * 16) = to_bf16x4(acc[i]);
+      }
+    }
   }
 }
 
@@ -545,33 +629,35 @@ __global__ __launch_bounds__(256) void paged_out_kernel(const PagedAttendArgs a)
 
 }  // namespace
 
-void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit) {
-  const int wide = paged_wide_rows(d_c, d_rope);
-  if (wide > 0 && max_rows > 32) {
+namespace {
+// 16-row blocks per workgroup of the few-row kernel: the most whose accumulators leave the registers room
+constexpr int few_most(int dc) { return dc <= 128 ? 4 : dc <= 192 ? 3 : 1; }
+}  // namespace
+
+void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit, int32_t* cost) {
+  const int wide = paged_wide_rows(d_c, d_rope), most = 16 * few_most(d_c);
+  if (wide > 0 && max_rows > most) {
     *rows = wide;
     *unit = 32;
+    *cost = 8;
     return;
   }
-  *rows = max_rows <= 16 ? 16 : 32;
+  *rows = max_rows <= 16 || most == 16 ? 16 : max_rows <= 32 ? 32 : most;
   *unit = 32 * few_waves(d_c);
-}
-
-hipError_t launch_paged_plan(const PagedAttendArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
-  return hipGetLastError();
+  *cost = 1;
 }
 
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
-  if (a.rows > 32) return launch_paged_attend_wide(a, s);
+  if (a.unit == 32) return launch_paged_attend_wide(a, s);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(a.n_wg), dim3(64 * few_waves(a.d_c)), 0, s, a);
+    return hipGetLastError();
+  };
 #define X(DC, DR)                                                                                     \
   if (a.d_c == DC && a.d_rope == DR) {                                                                \
-    if (a.rows == 16)                                                                                 \
-      hipLaunchKernelGGL((paged_attend_few_kernel<DC, DR, 1>), dim3(a.n_wg),                          \
-                         dim3(64 * few_waves(DC)), 0, s, a);                                          \
-    else                                                                                              \
-      hipLaunchKernelGGL((paged_attend_few_kernel<DC, DR, 2>), dim3(a.n_wg),                          \
-                         dim3(64 * few_waves(DC)), 0, s, a);                                          \
-    return hipGetLastError();                                                                         \
+    if (a.rows == 16) return go(paged_attend_few_kernel<DC, DR, 1>);                                  \
+    if (a.rows == 32) return go(paged_attend_few_kernel<DC, DR, (few_most(DC) > 1 ? 2 : 1)>);         \
+    return go(paged_attend_few_kernel<DC, DR, few_most(DC)>);                                         \
   }
   VMLA_PAGED_SHAPES(X)
 #undef X
@@ -579,14 +665,16 @@ hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s) {
-#define X(DC, DR)                                                                                     \
-  if (a.d_c == DC && a.d_rope == DR) {                                                                \
-    if (a.pg.n_tokens <= 128)                                                                         \
-      hipLaunchKernelGGL((paged_out_kernel<DC, 1>), dim3(a.pg.n_tokens, a.n_heads), dim3(256), 0, s, a); \
-    else                                                                                              \
-      hipLaunchKernelGGL((paged_out_kernel<DC, 16>), dim3((a.pg.n_tokens + 15) / 16, a.n_heads),      \
-                         dim3(256), 0, s, a);                                                         \
-    return hipGetLastError();                                                                         \
+  const int n = a.pg.n_tokens;
+  auto go = [&](auto kernel, int tg) {
+    hipLaunchKernelGGL(kernel, dim3((n + tg - 1) / tg, a.n_heads), dim3(256), 0, s, a);
+    return hipGetLastError();
+  };
+#define X(DC, DR)                                                       \
+  if (a.d_c == DC && a.d_rope == DR) {                                  \
+    if (n <= 128) return go(paged_out_kernel<DC, 1>, 1);                \
+    if (n <= 1024 || DC > 256) return go(paged_out_kernel<DC, 16>, 16); \
+    return go(paged_out_kernel<DC, (DC > 256 ? 16 : 64)>, 64);            \
   }
   VMLA_PAGED_SHAPES(X)
 #undef X

@@ -49,9 +49,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const int g = lane >> 5, l32 = lane & 31;
   const PagedGeo& pg = a.pg;
   const int H = a.n_heads;
-  const PagedWork wk = a.plan.work[blockIdx.x];
-  int left = __builtin_amdgcn_readfirstlane(wk.n_units);
-  int blk = __builtin_amdgcn_readfirstlane(wk.block), end = __builtin_amdgcn_readfirstlane(wk.end);
+  const PagedWork wk = paged_read<true>(a.plan.work, blockIdx.x);
+  int left = wk.n, blk = wk.block, end = wk.end;
 
   // this wave's loads j = wave + NW i of a tile: in bits 0..15 the offset of this lane's chunk in its row's
   // c_kv, or (bit 31) k_r (the pad reads k_r again, against zeros in q_cat), in bits 16..20 the tile row
@@ -71,23 +70,23 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const int vofs_lo = C::at(4 * g + tr_row, tr_col), vofs_hi = C::at(4 * g + tr_row + 8, tr_col);
 
   while (left > 0) {
-    const PagedBlock pb = a.plan.block[blk];
-    const int seq = __builtin_amdgcn_readfirstlane(pb.seq);
-    const int n_units = __builtin_amdgcn_readfirstlane(pb.n_units);
-    if (end == 0) end = n_units;  // a segment before the workgroup's last ends with its block
-    const int n_tiles = min(left, end), u0 = end - n_tiles;
-    const int row0 = __builtin_amdgcn_readfirstlane(pb.row0) + wave * 32;
-    const int key0 = __builtin_amdgcn_readfirstlane(pb.key0) + u0 * 32;
-    const PagedSeq sq = paged_seq<true>(pg, seq);
-    const int n_rows = (sq.hi - sq.lo) * H, base = sq.kv - (sq.hi - sq.lo);
-    const int32_t* table = pg.table + (int64_t)seq * pg.max_pages;
+    const PagedBlock pb = paged_read<true>(a.plan.block, blk);
+    if (end < 0) end = pb.n_units + a.cost;  // a block before the workgroup's last is taken to its end
+    const int len = min(left, end), u1 = end - a.cost, u0 = max(u1 - len, 0), n_tiles = u1 - u0;
+    left -= len;
+    end = -1;
+    --blk;
+    if (n_tiles <= 0) continue;
+    const int row0 = pb.row0 + wave * 32, n_rows = pb.n_rows;
+    const int key0 = pb.key0 + u0 * 32;
+    const int32_t* table = pg.table + (int64_t)pb.seq * pg.max_pages;
     __syncthreads();  // the previous segment's tiles are no longer read
 
     // page ids of tile t's keys, one per lane (a key outside the sequence reads the nearest entry)
     auto load_id = [&](int t) { return table[page_of(pg, min(key0 + t * 32 + l32, pg.max_kv - 1))]; };
     auto row_of = [&](int t, int32_t page) {  // this lane's key's pool row, -1: none, or past the segment
       const int key = key0 + t * 32 + l32;
-      if (t >= n_tiles || key >= sq.kv || page < 0 || page >= pg.n_pages) return -1;
+      if (t >= n_tiles || key >= pb.kv || page < 0 || page >= pg.n_pages) return -1;
       return page * pg.page_tokens + key - page_of(pg, key) * pg.page_tokens;
     };
     auto load_tile = [&](int row, uint16_t* buf) {
@@ -120,32 +119,23 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     const int r_own = row0 + l32;
     {
       const bool live = r_own < n_rows;
-      const uint16_t* src = a.qcat + ((int64_t)sq.lo * H + (live ? r_own : 0)) * C::DQKP + 8 * g;
+      const uint16_t* src = a.qcat + ((int64_t)pb.lo * H + (live ? r_own : 0)) * C::DQKP + 8 * g;
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
         u32x4 v = ldg16(src + ks * 16);
         if (!live) v = u32x4{0, 0, 0, 0};
         q[ks] = as_bf16x8(v);
       }
-      if (live) paged_seen(pg, sq, base + r_own / H, see_b, see_e);
+      if (live) paged_row_sees(pg, pb, H, wave * 32 + l32, see_b, see_e);
     }
-    // rows are in token order: the limits of the wave's, and of the block's, first and last row hold for all
-    const int last = min(n_rows - 1 - row0, 31);
-    const int b_max = __builtin_amdgcn_readlane(see_b, max(last, 0));
+    // rows are in token order: the limits of the wave's first and last row hold for all
+    const int b_max = __builtin_amdgcn_readlane(see_b, max(min(n_rows - 1 - row0, 31), 0));
     const int e_min = __builtin_amdgcn_readfirstlane(see_e);
-    int blk_b, blk_e, unused;
-    {
-      const int first_row = __builtin_amdgcn_readfirstlane(pb.row0);
-      paged_seen(pg, sq, base + (min(first_row + C::ROWS, n_rows) - 1) / H, blk_b, unused);
-      paged_seen(pg, sq, base + first_row / H, unused, blk_e);
-      blk_b = __builtin_amdgcn_readfirstlane(blk_b);
-      blk_e = __builtin_amdgcn_readfirstlane(blk_e);
-    }
     // the latents of tile t in buf, made finite if some row of the block does not see one of its keys
     // (called by all waves, after every wave has used the tile's K and before any uses its V)
     auto settle = [&](int t, uint16_t* buf) {
       const int k0 = key0 + t * 32;
-      if (k0 >= blk_b && k0 + 32 <= blk_e) return;
+      if (k0 >= pb.all_b && k0 + 32 <= pb.all_e) return;
       for (int i = threadIdx.x; i < 32 * C::CPR; i += NW * 64) {
         u32x4* p = reinterpret_cast<u32x4*>(buf + i * 8);
         *p = as_u32x4(finite_or_zero(as_bf16x8(*p)));
@@ -299,10 +289,10 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       // ---- a whole block's latents, or this segment's partial result ----
       const float l = half_swap_sum(l_run);
       if (r_own < n_rows) {
-        const bool whole = n_tiles == n_units;
+        const bool whole = n_tiles == pb.n_units;
         const int64_t prow = (2 * (int64_t)blockIdx.x + (u0 == 0)) * C::ROWS + wave * 32 + l32;
         const float f = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;  // (a row that sees nothing: zeros)
-        float* dst = whole ? a.o_lat + ((int64_t)sq.lo * H + r_own) * DC : a.o_part + prow * DC;
+        float* dst = whole ? a.o_lat + ((int64_t)pb.lo * H + r_own) * DC : a.o_part + prow * DC;
 #pragma unroll
         for (int d = 0; d < C::DVB; ++d)
 #pragma unroll
@@ -318,9 +308,6 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
         }
       }
     }
-    left -= n_tiles;
-    end = 0;
-    --blk;
   }
 }
 

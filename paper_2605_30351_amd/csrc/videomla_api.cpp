@@ -153,7 +153,7 @@ enum KernelId {
   K_MAT_KV, K_MAT_Q_PREP, K_MAT_ATTEND, K_MAT_MERGE,
   K_DENSE_Q_PREP, K_DENSE_ATTEND, K_DENSE_MERGE,
   K_Q_DOWN, K_Q_UP, K_LATENT_MERGE, K_OUT_MIX, K_CACHE_WRITE, K_DENSE_CACHE_WRITE,
-  K_PAGED_PLAN, K_PAGED_ABSORB, K_PAGED_ATTEND, K_PAGED_OUT, K_PAGED_CACHE_WRITE, K_COUNT
+  K_PAGED_ABSORB, K_PAGED_ATTEND, K_PAGED_OUT, K_PAGED_CACHE_WRITE, K_COUNT
 };
 const char* kKernelNames[K_COUNT] = {"q_absorb",     "latent_attend", "out_proj",
                                      "rope_window",  "bal_prep",      "mat_kv",
@@ -161,8 +161,8 @@ const char* kKernelNames[K_COUNT] = {"q_absorb",     "latent_attend", "out_proj"
                                      "dense_q_prep", "dense_attend",  "dense_merge",
                                      "q_down",       "q_up",          "latent_merge",
                                      "out_mix",      "cache_write",   "dense_cache_write",
-                                     "paged_plan",   "paged_absorb",  "paged_attend",
-                                     "paged_out",    "paged_cache_write"};
+                                     "paged_absorb", "paged_attend",  "paged_out",
+                                     "paged_cache_write"};
 
 int kernel_id(const char* name) {
   for (int k = 0; k < K_COUNT; ++k)
@@ -1067,8 +1067,8 @@ PagedGeo make_paged_geo(const videomla_dims* d, const videomla_paged* p) {
 // Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots, the
 // plan and the row of zeros.
 struct PagedLayout {
-  size_t qcat, o_lat, o_part, ml, zero, head, seq_block, block, first_unit, work, total;
-  int32_t rows, unit, max_blocks, n_wg;
+  size_t qcat, o_lat, o_part, ml, zero, head, seq_block, block, first, work, total;
+  int32_t rows, unit, cost, max_blocks, n_wg;
 };
 
 int check_paged_attend_shape(const videomla_dims* d, const videomla_paged* p) {
@@ -1083,7 +1083,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
   PagedLayout L{};
   const int64_t rows = (int64_t)p->n_tokens * d->n_heads;
   const int64_t max_new = p->max_new > 0 && p->max_new < p->n_tokens ? p->max_new : p->n_tokens;
-  paged_attend_shape(d->d_c, d->d_rope, max_new * d->n_heads, &L.rows, &L.unit);
+  paged_attend_shape(d->d_c, d->d_rope, max_new * d->n_heads, &L.rows, &L.unit, &L.cost);
   // a sequence's last block may be partly filled; sequences without rows have none
   L.max_blocks = (int32_t)(rows / L.rows + (p->n_seqs < p->n_tokens ? p->n_seqs : p->n_tokens));
   L.n_wg = device_cu_count();
@@ -1102,7 +1102,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
   L.head = take(2 * sizeof(int64_t));
   L.seq_block = take(((size_t)p->n_seqs + 1) * sizeof(int32_t));
   L.block = take((size_t)L.max_blocks * sizeof(PagedBlock));
-  L.first_unit = take(((size_t)L.max_blocks + 1) * sizeof(int64_t));
+  L.first = take(((size_t)L.max_blocks + 1) * sizeof(int64_t));
   L.work = take((size_t)L.n_wg * sizeof(PagedWork));
   L.total = at;
   return L;
@@ -1166,9 +1166,9 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   a.plan.head = reinterpret_cast<int64_t*>(ws + L.head);
   a.plan.seq_block = reinterpret_cast<int32_t*>(ws + L.seq_block);
   a.plan.block = reinterpret_cast<PagedBlock*>(ws + L.block);
-  a.plan.first_unit = reinterpret_cast<int64_t*>(ws + L.first_unit);
+  a.plan.first = reinterpret_cast<int64_t*>(ws + L.first);
   a.plan.work = reinterpret_cast<PagedWork*>(ws + L.work);
-  a.max_blocks = L.max_blocks; a.rows = L.rows; a.unit = L.unit;
+  a.max_blocks = L.max_blocks; a.rows = L.rows; a.unit = L.unit; a.cost = L.cost;
   a.batch = 1; a.n_heads = d->n_heads; a.d_nope = d->d_nope; a.d_rope = d->d_rope;
   a.d_c = d->d_c; a.d_v = d->d_v;
   a.dqk_pad = (int32_t)round_up((size_t)d->d_c + d->d_rope, 16);
@@ -1180,9 +1180,7 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
                                               : 1.0 / std::sqrt((double)d->d_nope + d->d_rope);
   a.qscale = (float)(scale * 1.4426950408889634);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  hipError_t e = timed(p->timer, K_PAGED_PLAN, s, [&] { return launch_paged_plan(a, s); });
-  if (e != hipSuccess) return hip_fail(e, "paged_plan");
-  e = timed(p->timer, K_PAGED_ABSORB, s, [&] { return launch_paged_absorb(a, s); });
+  hipError_t e = timed(p->timer, K_PAGED_ABSORB, s, [&] { return launch_paged_absorb(a, s); });
   if (e != hipSuccess) return hip_fail(e, "paged_absorb");
   e = timed(p->timer, K_PAGED_ATTEND, s, [&] { return launch_paged_attend(a, s); });
   if (e != hipSuccess) return hip_fail(e, "paged_attend");

@@ -50,7 +50,11 @@ struct PagedSeq {
 // scalar load, which does not wait for the vector loads in flight.
 template <bool UNIFORM, class T>
 __device__ __forceinline__ T paged_read(const T* p, int64_t i) {
-  if constexpr (UNIFORM) {
+  if constexpr (UNIFORM && sizeof(T) > 8) {
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
+    typedef const __attribute__((address_space(4))) words* scalar_ptr;
+    return __builtin_bit_cast(T, *(scalar_ptr)(uintptr_t)(p + i));
+  } else if constexpr (UNIFORM) {
     typedef const __attribute__((address_space(4))) T* scalar_ptr;
     return *(scalar_ptr)(uintptr_t)(p + i);
   } else {
@@ -80,6 +84,29 @@ __device__ __forceinline__ int paged_seq_of(const PagedGeo& g, int t) {
   return lo < g.n_seqs && t >= g.cu[lo] ? lo : -1;
 }
 
+// The same for a token row per lane (all lanes of the wave take part): the first 64 steps of the search
+// come from one load, a lane each, and the rest, for more than 64 sequences, from memory.
+__device__ __forceinline__ int paged_seq_of_lanes(const PagedGeo& g, int t) {
+  const int lane = threadIdx.x & 63, stride = (g.n_seqs + 63) >> 6;
+  const int end = g.cu[min((lane + 1) * stride, g.n_seqs)];  // end of the lane's group of sequences
+  int c = 0;  // groups that end at or before row t
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1)
+    if (__shfl(end, c + d - 1) <= t) c += d;
+  if (__shfl(end, c) <= t) ++c;
+  int lo = min(c * stride, g.n_seqs), hi = min(lo + stride, g.n_seqs);
+  if (stride == 1) {
+    hi = lo;
+  } else {
+    while (lo < hi) {
+      const int m = (lo + hi) >> 1;
+      if (g.cu[m + 1] > t) hi = m;
+      else lo = m + 1;
+    }
+  }
+  return lo < g.n_seqs && t >= g.cu[lo] ? lo : -1;
+}
+
 // The pool row of cached token j, -1 for a hole (j outside the sequence, or its page outside the pool).
 __device__ __forceinline__ int32_t paged_row(const PagedGeo& g, int s, int32_t kv, int32_t j) {
   if (j < 0 || j >= kv) return -1;
@@ -98,20 +125,21 @@ __device__ __forceinline__ void paged_pos(const PagedGeo& g, int64_t pos, int64_
   x = r - y * g.grid_w;
 }
 
-// The cached tokens [b, e) that the query at cached index i sees (i < 0: a row before the cached
-// tokens): keys below the end of the query's mask block and, with a window, at most that many below it.
-__device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q, int32_t i, int32_t& b,
-                                           int32_t& e) {
-  int64_t end = q.kv;
+// What the query at cached index i sees (i < 0: a row before the cached tokens), not clamped to the
+// cached tokens: keys below the end of the query's mask block and, with a window, at most that many below
+// it. to_next: tokens to the next mask block.
+__device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q, int32_t i, int64_t& beg,
+                                           int64_t& end, int64_t& to_next) {
+  end = q.kv;
+  to_next = kPagedFar;
   if (g.mask_block > 0) {
     const int64_t p = q.first + i;  // floor division: rows before position 0 count down
     int64_t blk = p / g.mask_block;
     if (p - blk * g.mask_block < 0) --blk;
-    end = (blk + 1) * g.mask_block - q.first;
+    to_next = (blk + 1) * g.mask_block - p;
+    end = i + to_next;
   }
-  const int64_t beg = g.window > 0 ? end - g.window : 0;
-  e = (int32_t)(end < 0 ? 0 : end > q.kv ? q.kv : end);
-  b = (int32_t)(beg < 0 ? 0 : beg > e ? e : beg);
+  beg = g.window > 0 ? end - g.window : -kPagedFar;
 }
 
 // The running maximum starts at the lowest finite value, not at -inf: a row that has seen nothing yet
@@ -134,29 +162,51 @@ __device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 v) {
   return as_bf16x8(u);
 }
 
-// The plan of one attention call, in the workspace: written by paged_plan_kernel, read by the
-// attention and the output kernels of the same call.
+// The plan of one attention call, in the workspace: written beside the absorbed queries (paged_plan),
+// read by the attention and the output kernels of the same call.
 //   Row blocks: the (token, head) rows of a sequence in blocks of R, sequences in order. A block's keys
-//   are the tiles that some of its rows see: `n_units` units of `unit` keys from `key0` (a block that
-//   sees nothing keeps one unit: it still writes its rows).
-//   Work: the units of all blocks in order, split evenly over G workgroups; workgroup w takes
-//   [w U / G, (w + 1) U / G). Consecutive units of one block are a segment. A block inside one workgroup
-//   is written as its latents; of a split one each workgroup leaves a partial result, in slot 2 w + 1
-//   for the block's first segment and 2 w for a later one (a workgroup has at most one of each). A
-//   workgroup takes its segments last to first: all ranges are equally long, the last segment starts at
-//   a block's first key and the first ends at a block's last, so that the workgroups walk the keys of a
-//   sequence at about the same place at the same time and find tiles in their XCD's L2.
+//   are the units of `unit` keys from `key0` that some of its rows see (a block that sees nothing keeps
+//   one: it still writes its rows).
+//   Work: every block counts as its units and `cost` more, which stand for what a workgroup spends on
+//   entering and leaving a block. The blocks in order are split evenly over G workgroups by these counts:
+//   workgroup w takes counts [w U / G, (w + 1) U / G), and of a block the units behind its first `cost`
+//   counts. A block inside one workgroup is written as its latents; of a split one each workgroup leaves
+//   a partial result, in slot 2 w + 1 for the block's first unit and 2 w for a later start (a workgroup
+//   has at most one of each). A workgroup takes its blocks last to first: all ranges are about equally
+//   long, the last block's part starts at its first key and the first block's ends at its last, so that
+//   the workgroups walk the keys of a sequence at about the same place at the same time and find tiles
+//   in their XCD's L2.
 struct PagedBlock {
-  int32_t seq, row0, key0, n_units;
+  int32_t seq, row0, key0, n_units;  // sequence, first row in it, first key (a multiple of 32), units
+  int32_t lo, n_rows, kv;            // the sequence's first token row, its rows, its cached tokens
+  int32_t head0;                     // head of the first row
+  int32_t all_b, all_e;              // the keys [all_b, all_e) that all rows of the block see
+  int32_t to_next;                   // tokens from the first row's to the next mask block (saturated)
+  int32_t pad;
+  int64_t beg0, end0;                // the first row's keys, not clamped to the cached tokens
 };
+static_assert(sizeof(PagedBlock) == 64, "one scalar load");
+
+// The keys [b, e) that row r of the block (counted from its first row) sees. A block's rows are at most
+// 256 tokens, so that only mask blocks below that length are crossed more than once.
+__device__ __forceinline__ void paged_row_sees(const PagedGeo& g, const PagedBlock& p, int H, int r,
+                                               int32_t& b, int32_t& e) {
+  const int d = (p.head0 + r) / H - p.to_next;  // tokens past the first boundary
+  int64_t off = 0;
+  if (d >= 0) off = (1 + (g.mask_block <= 256 ? d / (int)g.mask_block : 0)) * g.mask_block;
+  const int64_t end = p.end0 + off, beg = p.beg0 + off;
+  e = (int32_t)(end < 0 ? 0 : end > p.kv ? p.kv : end);
+  b = (int32_t)(beg < 0 ? 0 : beg > e ? e : beg);
+}
+
 struct PagedWork {
-  int32_t block, end, n_units, pad;  // last row block, the end in its units, units of the workgroup
+  int32_t block, end, n, pad;  // last row block, the end in its counts, counts of the workgroup
 };
 struct PagedPlan {
-  int64_t* head;        // [2]: units U, workgroups G in use
+  int64_t* head;        // [2]: counts U, workgroups G in use
   int32_t* seq_block;   // [n_seqs + 1] first row block of each sequence
   PagedBlock* block;    // [max_blocks]
-  int64_t* first_unit;  // [max_blocks + 1]
+  int64_t* first;       // [max_blocks + 1] first count of each block
   PagedWork* work;      // [n_wg]
 };
 
@@ -171,18 +221,18 @@ struct PagedAttendArgs : AttendArgs {
   uint16_t* zero_row;  // workspace: a row of zeros, staged in a hole's place
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
+  int32_t cost;        // counts of a block beyond its units
 };
 
 constexpr int kPagedMaxSeqs = 4096;
 
 hipError_t launch_paged_cache_write(const PagedWriteArgs& a, hipStream_t s);
 hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s);
-hipError_t launch_paged_plan(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s);
 
 // Rows per block and keys per unit of the attention kernel for sequences of at most max_rows rows.
-void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit);
+void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit, int32_t* cost);
 // The kernel of many rows per block (k_paged_wide.hip): its block, 0 where it is not built, and launch.
 int paged_wide_rows(int d_c, int d_rope);
 hipError_t launch_paged_attend_wide(const PagedAttendArgs& a, hipStream_t s);
