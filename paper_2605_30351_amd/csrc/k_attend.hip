@@ -44,10 +44,11 @@ template <int DC> struct AbsorbChunk {  // W_UK_h columns staged in LDS per pass
 // all token rows), each at its sequence's own position; the first workgroup makes the call's plan.
 template <int DC, int DR, class Args>
 __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
+  extern __shared__ __attribute__((aligned(16))) uint16_t wuk[];  // [d_nope][WS]
   constexpr bool PAGED = std::is_same<Args, PagedAttendArgs>::value;
   if constexpr (PAGED) {
     if (blockIdx.x == 0) {
-      if (blockIdx.y == 0) paged_plan(a);
+      if (blockIdx.y == 0) paged_plan(a, wuk);
       return;
     }
   }
@@ -58,7 +59,6 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   constexpr int DQKP = (DC + DR + 15) / 16 * 16;
   constexpr int NCB = CW / 32;
   constexpr int KN = kMaxNope / 16;
-  extern __shared__ __attribute__((aligned(16))) uint16_t wuk[];  // [d_nope][WS]
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -102,7 +102,9 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
   // its position would otherwise be repeated by every lane that rotates one of its pairs)
   __shared__ double qpos[4][3][32];
   int seq = -1;
-  if constexpr (PAGED) seq = paged_seq_of_lanes(a.pg, min(tok0 + lane, Nq - 1));
+  if constexpr (PAGED) {
+    seq = paged_seq_of_lanes(a.pg, min(tok0 + lane, Nq - 1));
+  }
   if (lane < 32) {
     TokenPos tp{};
     if constexpr (PAGED) {
@@ -214,6 +216,9 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
         else a.qcat[r * DQKP + c] = 0;
       }
     }
+  }
+  if constexpr (PAGED) {
+    if (lane < 32 && ok) a.plan.row[row] = PagedRow{};
   }
   VMLA_STAMP(a, kStampQAbsorb, 4);
   if constexpr (STAGE) {
@@ -1217,9 +1222,10 @@ hipError_t launch_q_absorb(const AttendArgs& a, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s) {
+hipError_t launch_paged_absorb_tiles(const PagedAttendArgs& a, hipStream_t s) {
   const dim3 grid((a.pg.n_tokens + 127) / 128 + 1, a.n_heads);
-  const size_t lds = q_absorb_lds_bytes(a.d_c, a.d_rope, a.d_nope);
+  size_t lds = q_absorb_lds_bytes(a.d_c, a.d_rope, a.d_nope);
+  if (lds < (size_t)kPlanLds) lds = kPlanLds;
 #define X(DC, DR)                                                                            \
   if (a.d_c == DC && a.d_rope == DR) {                                                       \
     hipLaunchKernelGGL((q_absorb_kernel<DC, DR, PagedAttendArgs>), grid, dim3(256), lds, s, a); \

@@ -122,7 +122,8 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
   }
 
   while (left > 0) {
-    const PagedBlock pb = paged_read<true>(a.plan.block, blk);
+    const bool last = blk == wk.block;  // (whose record the plan has copied: one load less in line)
+    const PagedBlock pb = last ? paged_read<true>(a.plan.work_block, blockIdx.x) : paged_read<true>(a.plan.block, blk);
     if (end < 0) end = pb.n_units + a.cost;  // a block before the workgroup's last is taken to its end
     const int len = min(left, end), u1 = end - a.cost, u0 = max(u1 - len, 0), take = u1 - u0;
     left -= len;
@@ -140,6 +141,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       lds_dma4(table + page_of(g, key), __builtin_amdgcn_readfirstlane(lds_addr(&ids[wave][t & 1][0])));
     };
     load_ids(0);
+    load_ids(1);
 
     // this lane's rows and what they see
     bf16x8 qv[C::QLDS ? 1 : QB][C::KS];
@@ -183,16 +185,17 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       const int key = key0 + t * C::UNIT + (lane & 31);
       // (through an LDS pointer: a generic one would wait for every load in flight)
       const int32_t page = *(const volatile lds_i32*)(&ids[wave][t & 1][lane]);
-      if (key >= pb.kv || page < 0 || page >= g.n_pages) return -1;
-      return page * g.page_tokens + key - page_of(g, key) * g.page_tokens;
+      const int row = page * g.page_tokens + key - page_of(g, key) * g.page_tokens;
+      return key < pb.kv && (uint32_t)page < (uint32_t)g.n_pages ? row : -1;
     };
     auto load_tile = [&](int t, int row) {
+      const int at_row = max(row, 0);  // in a missing key's place, the pool's first row: masked, made finite
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(&tiles[wave][t & 1][0]));
       if constexpr (C::SPLIT) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          const int32_t r = __builtin_amdgcn_readlane(row, j);
-          lds_dma16_row(r < 0 ? a.zero_row : a.c_kv + (int64_t)r * DC, (lane ^ C::swz16(j)) * 16, lds + 1024u * j);
+          const uint32_t r = __builtin_amdgcn_readlane(at_row, j);
+          lds_dma16_row(a.c_kv + (uint64_t)r * DC, (lane ^ C::swz16(j)) * 16, lds + 1024u * j);
         }
       }
 #pragma unroll
@@ -201,11 +204,10 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
         uint32_t at = d_at[j % NAT];
         // recomputed from one register a load: kept across the loop, the addresses' parts would fill the file
         if constexpr (QB * DC >= 256) asm volatile("" : "+v"(at));
-        const int32_t r = __shfl(row, (int)(at >> 16 & 15) + 16 * half);
+        const uint32_t r = __shfl(at_row, (int)(at >> 16 & 15) + 16 * half);
         const bool kr = (int32_t)at < 0;
-        const uint16_t* p = kr ? a.k_r : a.c_kv;
-        p += (int64_t)r * (kr ? DR : DC) + (at & 0xffffu);
-        lds_dma16(r < 0 ? a.zero_row : p, lds + 1024u * j);
+        const uint16_t* p = (kr ? a.k_r : a.c_kv) + (at & 0xffffu);
+        lds_dma16(p + (uint64_t)r * (uint32_t)(kr ? DR : DC), lds + 1024u * j);
       }
     };
 
@@ -243,22 +245,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       else return qv[qb][ks];
     };
 
-    wait_loads<0>();
-    int row = row_of(0);
-    load_ids(1);
-    load_tile(0, row);
-    for (int t = 0; t < take; ++t) {
-      const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);  // keys of tile t that exist
-      if (t + 1 < take) {
-        wait_loads<C::NDMA>();  // the ids of tile t + 1
-        row = row_of(t + 1);
-        load_ids(t + 2);
-        load_tile(t + 1, row);
-        wait_loads<C::NDMA + 1>();  // tile t
-      } else {
-        wait_loads<0>();
-      }
-      if (there == 0) continue;
+    auto use_tile = [&](int t, uint32_t there) {
       const int k0 = key0 + t * C::UNIT;
       const uint16_t* tile = tiles[wave][t & 1];
       const bool masked = there != 0xffffffffu || k0 < pb.all_b || k0 + 32 > pb.all_e;
@@ -279,15 +266,12 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       }
       if (masked) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
+        for (int qb = 0; qb < QB; ++qb) {
+          const uint32_t seen = seen_keys(there, see_b[qb] - k0, see_e[qb] - k0) >> (4 * gq);
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int k = 16 * kb + 4 * gq + i;
-              const bool seen = (there >> k & 1) && k0 + k >= see_b[qb] && k0 + k < see_e[qb];
-              s[qb][kb][i] = seen ? s[qb][kb][i] : kMasked;
-            }
+          for (int i = 0; i < 8; ++i)
+            s[qb][i >> 2][i & 3] = seen >> (16 * (i >> 2) + (i & 3)) & 1 ? s[qb][i >> 2][i & 3] : kMasked;
+        }
       }
       float own[QB];
       bool grow = false;
@@ -341,12 +325,35 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       };
       if (masked) pv(std::true_type{});
       else pv(std::false_type{});
+    };
+
+    wait_loads<0>();
+    int row = row_of(0), row_n = row_of(1);
+    load_tile(0, row);
+    load_ids(2);
+    if (take > 1) load_tile(1, row_n);
+    // outstanding at the top of iteration t: the loads of tile t, the ids of tile t + 2, the loads of t + 1
+    for (int t = 0; t < take; ++t) {
+      const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0);  // keys of tile t that exist
+      if (t + 1 < take) wait_loads<C::NDMA + 1>();
+      else wait_loads<0>();
+      if (there != 0) use_tile(t, there);
+      row = row_n;
+      if (t + 2 < take) {
+        wait_loads<C::NDMA>();  // the ids of tile t + 2
+        row_n = row_of(t + 2);
+        load_ids(t + 3);
+        load_tile(t + 2, row_n);  // into tile t's buffer: its values are in registers
+      }
     }
 
     // ---- the waves' results, merged in wave order, 16 QP rows at a time ----
     float* res = reinterpret_cast<float*>(&tiles[wave][0][0]);  // [16 QP][RS]: this wave's own buffers
     const bool whole = take == pb.n_units;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (u0 == 0);
+    if (u0 == 0 && (int)threadIdx.x < C::ROWS && row0 + (int)threadIdx.x < n_rows)
+      a.plan.row[(int64_t)pb.lo * H + row0 + threadIdx.x] =
+          PagedRow{(int32_t)blockIdx.x, (uint16_t)(last ? wk.last_ns : 1), (uint16_t)threadIdx.x};
 #pragma unroll
     for (int q0 = 0; q0 < QB; q0 += C::QP) {
 #pragma unroll
@@ -395,207 +402,112 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
 }
 
 // ---- merge and value up-projection -------------------------------------------------------------
-// grid (ceil(n_tokens / TG), H), 256 threads: the latents of TG tokens of one head, merged where their
-// row block was split, then out^T[v][token] = W_UV_h[v][:] . o_lat[token][:]. The latents go into the
-// product as two bf16 terms (16 bits of fraction): one alone adds a rounding as large as the output's
+// out[token, h] = W_UV_h o_lat[token, h], o_lat merged where its row block was split. The latents go into
+// the product as two bf16 terms (16 bits of fraction): one alone adds a rounding as large as the output's
 // own, 2^-8 of the value, for a product that costs next to nothing here.
-// TG = 1 (few tokens: single-token steps, whose rows are split the most): the splits are read by slices
-// of the workgroup side by side, each with its own running maximum. More tokens: the coefficient of
-// every (token, split) goes into a table, and a thread sums its chunks, four in flight per split.
-constexpr int kOutSplits = 8;  // splits the table holds; tokens of more are merged one split after the other
+__device__ __forceinline__ void two_terms(f32x8 v, bf16x8& hi, bf16x8& lo) {
+  hi = to_bf16x8(v);
+  lo = to_bf16x8(v - __builtin_convertvector(hi, f32x8));
+}
+// Partial row of split k of a row (its first partial has the first key: slot 2 w + 1).
+__device__ __forceinline__ int64_t paged_part_row(const PagedAttendArgs& a, const PagedRow& r, int k) {
+  return (2 * (int64_t)(r.w0 + k) + (k == 0)) * a.rows + r.row;
+}
 
-template <int DC, int TG>
-__global__ __launch_bounds__(256, DC <= 256 ? 3 : 2) void paged_out_kernel(const PagedAttendArgs a) {
-  constexpr int LS = (DC > 32 ? DC : 32) + 8;  // LDS row stride (elements)
+// Few tokens (single-token steps, whose rows are split the most): a workgroup per row.
+// Slices of the workgroup merge the splits side by side, each with its own running maximum; a wave then
+// takes 16 of the d_v outputs at a time, whose weights are on their way meanwhile.
+template <int DC>
+__global__ __launch_bounds__(256) void paged_out_row_kernel(const PagedAttendArgs a) {
+  constexpr int LS = (DC > 32 ? DC : 32);
   constexpr int KS = (DC + 31) / 32;
-  constexpr int C4 = DC / 4;                   // 16-byte chunks of a partial row
-  constexpr int SL = TG > 1 ? 1 : 256 / C4 < 16 ? 256 / C4 : 16;  // slices of splits
-  constexpr int NB = (TG + 15) / 16;           // blocks of 16 tokens
-  __shared__ __attribute__((aligned(16))) uint16_t lat[2][TG][LS];  // o_lat's first and second term
+  constexpr int C4 = DC / 4;                           // 16-byte chunks of a partial row
+  constexpr int SL = 256 / C4 < 16 ? 256 / C4 : 16;    // slices
+  constexpr int AHEAD = DC > 256 ? 1 : 2;
+  __shared__ __attribute__((aligned(16))) uint16_t lat[2][LS];  // o_lat's first and second term
   __shared__ f32x4 part[SL][C4];
   __shared__ float part_m[SL], part_l[SL];
-  __shared__ float coef[TG > 1 ? TG : 1][kOutSplits];
-  __shared__ int32_t tok_row[TG], tok_w0[TG], tok_ns[TG], most_s;  // (ns 0: no token of a sequence)
-  const PagedGeo& g = a.pg;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, l16 = lane & 15;
-  const int H = a.n_heads, h = blockIdx.y, t0 = blockIdx.x * TG;
+  const int64_t row = blockIdx.x;
+  const int h = (int)(blockIdx.x % (unsigned)a.n_heads);
+  const PagedRow at = paged_read<true>(a.plan.row, row);
 
-  // the weights of the wave's first output blocks, on their way while the latents are merged
   const int n_vb = a.d_v / 16;
   auto weight = [&](int vb, int ks) {
     u32x4 x = {0, 0, 0, 0};
-    if (ks * 32 + 8 * gq < DC) x = ldg16(a.w_uv + ((int64_t)h * a.d_v + vb * 16 + l16) * DC + ks * 32 + 8 * gq);
+    if (ks * 32 + 8 * gq < DC)
+      x = ldg16(a.w_uv + ((int64_t)h * a.d_v + vb * 16 + l16) * DC + ks * 32 + 8 * gq);
     return as_bf16x8(x);
   };
-  constexpr int AHEAD = DC > 256 ? 1 : 2;
   bf16x8 wv[AHEAD][KS];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) wv[i][ks] = weight(min(wave * AHEAD + i, n_vb - 1), ks);
+  if (at.ns == 0) return;  // a row of no sequence
 
-  // partial row of split k of a token (its first partial has the first key: slot 2 w + 1)
-  auto part_row = [&](int w0, int k, int row) { return (2 * (int64_t)(w0 + k) + (k == 0)) * a.rows + row; };
-  if (wave == 0) {
-    const int t = t0 + min(lane, TG - 1);
-    const int s0 = paged_seq_of_lanes(g, t), s = t < g.n_tokens ? s0 : -1;
-    const int r = s >= 0 ? (t - max(g.cu[s], 0)) * H + h : 0;
-    const int blk = s >= 0 ? a.plan.seq_block[s] + r / a.rows : 0;
-    const bool known = s >= 0 && blk < a.plan.seq_block[g.n_seqs];  // (else offsets that go down)
-    int ns = 0, w0 = 0;
-    if (known) {
-      const int64_t U = a.plan.head[0], G = a.plan.head[1];
-      w0 = (int)floor_div((a.plan.first[blk] + a.cost + 1) * G - 1, U);
-      ns = (int)floor_div(a.plan.first[blk + 1] * G - 1, U) - w0 + 1;
-    }
-    int most = ns;
-    if constexpr (TG > 1) {
-      const int row = r % a.rows;
-      if (ns > 1 && ns <= kOutSplits) {
-        f32x2 ml[kOutSplits];
-#pragma unroll
-        for (int k = 0; k < kOutSplits; ++k)
-          ml[k] = *reinterpret_cast<const f32x2*>(a.ml_part + part_row(w0, min(k, ns - 1), row) * 2);
-        float m = kLowest, l = 0.f;
-#pragma unroll
-        for (int k = 0; k < kOutSplits; ++k) m = fmaxf(m, ml[k][0]);
-#pragma unroll
-        for (int k = 0; k < kOutSplits; ++k) l += k < ns ? fast_exp2(ml[k][0] - m) * ml[k][1] : 0.f;
-        const float il = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing: zeros)
-        if (lane < TG)
-#pragma unroll
-          for (int k = 0; k < kOutSplits; ++k) coef[lane][k] = k < ns ? fast_exp2(ml[k][0] - m) * il : 0.f;
-      } else if (lane < TG) {
-#pragma unroll
-        for (int k = 0; k < kOutSplits; ++k) coef[lane][k] = k == 0 ? 1.f : 0.f;
-      }
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
-    }
-    if (lane < TG) {
-      tok_ns[lane] = ns;
-      tok_row[lane] = r % a.rows;
-      tok_w0[lane] = w0;
-    }
-    if (lane == 0) most_s = most;
-  }
-  if constexpr (DC < 32) {
-    for (int i = tid; i < 2 * TG * LS; i += 256) (&lat[0][0][0])[i] = 0;
-  }
-  __syncthreads();
-  auto put = [&](int t, int c4, f32x4 v) {  // chunk c4 of token t's latents
+  auto put = [&](int c4, f32x4 v) {
     const bf16x4 hi = to_bf16x4(v);
-    const f32x4 rest = v - __builtin_convertvector(hi, f32x4);
-    *reinterpret_cast<bf16x4*>(&lat[0][t][c4 * 4]) = hi;
-    *reinterpret_cast<bf16x4*>(&lat[1][t][c4 * 4]) = to_bf16x4(rest);
+    *reinterpret_cast<bf16x4*>(&lat[0][c4 * 4]) = hi;
+    *reinterpret_cast<bf16x4*>(&lat[1][c4 * 4]) = to_bf16x4(v - __builtin_convertvector(hi, f32x4));
   };
-  // the online merge of chunk c of token t's partial results k0, k0 + SL, ..
-  auto merge = [&](int t, int c, int k0, float& m, float& l, f32x4& v) {
-    const int ns = tok_ns[t], w0 = tok_w0[t];
-    m = kLowest;
-    l = 0.f;
-    v = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k = k0; k < ns; k += 4 * SL) {
-      f32x2 ml[4];
-      f32x4 x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int kk = k + j * SL < ns ? k + j * SL : k;  // (past the last: read again, weighed by zero)
-        const int64_t row = part_row(w0, kk, tok_row[t]);
-        ml[j] = *reinterpret_cast<const f32x2*>(a.ml_part + row * 2);
-        x[j] = *reinterpret_cast<const f32x4*>(a.o_part + row * DC + c * 4);
-      }
-      float m1 = m;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) m1 = fmaxf(m1, ml[j][0]);
-      const float f = fast_exp2(m - m1);
-      l *= f;
-      v *= f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (k + j * SL < ns) {
-          const float fj = fast_exp2(ml[j][0] - m1);
-          l += fj * ml[j][1];
-          v += fj * x[j];
-        }
-      }
-      m = m1;
-    }
-  };
-  const int most = most_s;
-  if constexpr (TG == 1) {
-    if (most == 0) return;
-    if (most == 1) {
-      if (tid < C4) put(0, tid, *reinterpret_cast<const f32x4*>(a.o_lat + ((int64_t)t0 * H + h) * DC + tid * 4));
-    } else {
-      const int slice = tid / C4, c = tid % C4;
-      if (slice < SL) {
-        float m, l;
-        f32x4 v;
-        merge(0, c, slice, m, l, v);
-        part[slice][c] = v;
-        if (c == 0) {
-          part_m[slice] = m;
-          part_l[slice] = l;
-        }
-      }
-      __syncthreads();
-      if (tid < C4) {
-        float m = kLowest, l = 0.f;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < SL; ++k) m = fmaxf(m, part_m[k]);
-        for (int k = 0; k < SL; ++k) {
-          const float f = fast_exp2(part_m[k] - m);
-          l += part_l[k] * f;
-          v += part[k][tid] * f;
-        }
-        put(0, tid, v * (l == 0.f ? 0.f : 1.f / l));
-      }
-    }
+  if constexpr (DC < 32) {
+    if (tid < 32) lat[0][tid] = lat[1][tid] = 0;
+    __syncthreads();
+  }
+  if (at.ns == 1) {
+    if (tid < C4) put(tid, *reinterpret_cast<const f32x4*>(a.o_lat + row * DC + tid * 4));
   } else {
-    // chunk e = (token, 4 columns); a token of no sequence reads row 0 and is not stored
-    constexpr int N = (TG * C4 + 255) / 256, IN = N < 4 ? N : 4;
-    auto source = [&](int e, int k) {
-      const int t = min(e / C4, TG - 1), ns = tok_ns[t];
-      const float* p = ns <= 1 ? a.o_lat + ((int64_t)(ns == 0 ? 0 : t0 + t) * H + h) * DC
-                               : a.o_part + part_row(tok_w0[t], min(k, ns - 1), tok_row[t]) * DC;
-      return reinterpret_cast<const f32x4*>(p + e % C4 * 4);
-    };
-#pragma unroll 1
-    for (int i0 = 0; i0 < N; i0 += IN) {
-      f32x4 v[IN];
+    const int slice = tid / C4, c = tid % C4;
+    if (slice < SL) {
+      float m = kLowest, l = 0.f;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int k = slice; k < at.ns; k += 4 * SL) {
+        f32x2 ml[4];
+        f32x4 x[4];
 #pragma unroll
-      for (int i = 0; i < IN; ++i) v[i] = *source(tid + 256 * (i0 + i), 0);
-      if (most > 1) {
+        for (int j = 0; j < 4; ++j) {
+          const int64_t pr = paged_part_row(a, at, k + j * SL < at.ns ? k + j * SL : k);  // (past the last: not used)
+          ml[j] = *reinterpret_cast<const f32x2*>(a.ml_part + pr * 2);
+          x[j] = *reinterpret_cast<const f32x4*>(a.o_part + pr * DC + c * 4);
+        }
+        float m1 = m;
 #pragma unroll
-        for (int i = 0; i < IN; ++i) v[i] *= coef[min((tid + 256 * (i0 + i)) / C4, TG - 1)][0];
-        for (int k = 1; k < min(most, kOutSplits); ++k) {
-          f32x4 x[IN];
+        for (int j = 0; j < 4; ++j) m1 = fmaxf(m1, ml[j][0]);
+        const float f = fast_exp2(m - m1);
+        l *= f;
+        v *= f;
 #pragma unroll
-          for (int i = 0; i < IN; ++i) x[i] = *source(tid + 256 * (i0 + i), k);
-#pragma unroll
-          for (int i = 0; i < IN; ++i) {
-            const float f = coef[min((tid + 256 * (i0 + i)) / C4, TG - 1)][k];
-            if (f != 0.f) v[i] += f * x[i];
+        for (int j = 0; j < 4; ++j) {
+          if (k + j * SL < at.ns) {
+            const float fj = fast_exp2(ml[j][0] - m1);
+            l += fj * ml[j][1];
+            v += fj * x[j];
           }
         }
+        m = m1;
       }
-#pragma unroll
-      for (int i = 0; i < IN; ++i) {
-        const int e = tid + 256 * (i0 + i), t = e / C4;
-        if (e >= TG * C4) continue;
-        if (tok_ns[t] > kOutSplits) {
-          float m, l;
-          merge(t, e % C4, 0, m, l, v[i]);
-          v[i] *= l == 0.f ? 0.f : 1.f / l;
-        }
-        put(t, e % C4, v[i]);
+      part[slice][c] = v;
+      if (c == 0) {
+        part_m[slice] = m;
+        part_l[slice] = l;
       }
+    }
+    __syncthreads();
+    if (tid < C4) {
+      float m = kLowest, l = 0.f;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < SL; ++k) m = fmaxf(m, part_m[k]);
+      for (int k = 0; k < SL; ++k) {
+        const float f = fast_exp2(part_m[k] - m);
+        l += part_l[k] * f;
+        v += part[k][tid] * f;
+      }
+      put(tid, v * (l == 0.f ? 0.f : 1.f / l));  // (a row that sees nothing: zeros)
     }
   }
   __syncthreads();
-
   for (int vb = wave * AHEAD; vb < n_vb; vb += 4 * AHEAD) {
     if (vb != wave * AHEAD) {
 #pragma unroll
@@ -603,24 +515,117 @@ __global__ __launch_bounds__(256, DC <= 256 ? 3 : 2) void paged_out_kernel(const
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) wv[i][ks] = weight(min(vb + i, n_vb - 1), ks);
     }
-#pragma unroll 1
-    for (int nb = 0; nb < NB; ++nb) {
-      const int t = min(16 * nb + l16, TG - 1);
-      f32x4 acc[AHEAD] = {};
+    f32x4 acc[AHEAD] = {};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const bf16x8 b = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[k][t][ks * 32 + 8 * gq]));
+      for (int k = 0; k < 2; ++k) {
+        const bf16x8 b = as_bf16x8(*reinterpret_cast<const u32x4*>(&lat[k][ks * 32 + 8 * gq]));
 #pragma unroll
-          for (int i = 0; i < AHEAD; ++i) acc[i] = mfma16(wv[i][ks], b, acc[i]);
-        }
-      if (16 * nb + l16 < TG && tok_ns[t] > 0) {
-        uint16_t* dst = a.out + ((int64_t)(t0 + t) * H + h) * a.d_v + vb * 16 + 4 * gq;
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-          if (vb + i < n_vb) *reinterpret_cast<bf16x4*>(dst + i * 16) = to_bf16x4(acc[i]);
+        for (int i = 0; i < AHEAD; ++i) acc[i] = mfma16(wv[i][ks], b, acc[i]);
       }
+    if (l16 == 0) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (vb + i < n_vb)
+          *reinterpret_cast<bf16x4*>(a.out + row * a.d_v + (vb + i) * 16 + 4 * gq) = to_bf16x4(acc[i]);
+    }
+  }
+}
+
+// More tokens: 4 waves x 16 tokens of one head per workgroup. A lane holds 8 of every 32 latents of its
+// token, loaded as the B operand needs them (whole lines: four lanes a token) and merged over the splits
+// in registers; W_UV_h passes through LDS, 64 rows at a time, and is read by all waves. Two blocks of 16
+// tokens per wave halve the reads of W_UV_h, and the workgroups that fit a compute unit: 8,190 tokens x 12
+// heads 41 us against 34, 2,808 tokens with two to three splits a row 30 against 24.
+template <int DC>
+__global__ __launch_bounds__(256, DC <= 192 ? 4 : DC <= 256 ? 3 : 2) void paged_out_tiles_kernel(const PagedAttendArgs a) {
+  constexpr int KS = (DC + 31) / 32;
+  constexpr int LS = KS * 32 + 8;               // LDS row stride (elements): rows 16 bytes apart in banks
+  constexpr int VR = 64, CPR = KS * 4;          // W rows per pass, 16-byte chunks per row
+  constexpr int PER = VR * CPR / 256;           // W chunks per thread and pass
+  constexpr int YS = KS > 6 ? 4 : KS;           // k-steps of a further split in flight
+  __shared__ __attribute__((aligned(16))) uint16_t wl[VR * LS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int gq = lane >> 4, l16 = lane & 15;
+  const int H = a.n_heads, n = a.pg.n_tokens;
+  const int h = (int)(blockIdx.x % (unsigned)H);
+  const int t = ((int)(blockIdx.x / (unsigned)H) * 4 + wave) * 16 + l16;
+
+  u32x4 wv[PER];
+  auto load_w = [&](int v0) {  // (rows past d_v repeat the last; d_c = 16: the second half of a k-step is zero)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = tid + 256 * i, r = min(v0 + e / CPR, a.d_v - 1), c = e % CPR;
+      wv[i] = c * 8 < DC ? ldg16(a.w_uv + ((int64_t)h * a.d_v + r) * DC + c * 8) : u32x4{0, 0, 0, 0};
+    }
+  };
+  load_w(0);
+
+  const int64_t row = (int64_t)min(t, n - 1) * H + h;
+  const PagedRow at = a.plan.row[row];
+  const int ns = t < n ? at.ns : 0;
+  f32x8 x[KS];
+  auto load = [&](const float* p, int k0, auto& v) {  // the lane's latents of the k-steps from k0 on
+#pragma unroll
+    for (int ks = 0; ks < (int)(sizeof(v) / sizeof(v[0])); ++ks) {
+      const int c = (k0 + ks) * 32 + 8 * gq;
+      f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+      if (DC % 32 == 0 || c < DC) {
+        lo = *reinterpret_cast<const f32x4*>(p + c);
+        hi = *reinterpret_cast<const f32x4*>(p + c + 4);
+      }
+      v[ks] = f32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  };
+  load(ns <= 1 ? a.o_lat + row * DC : a.o_part + paged_part_row(a, at, 0) * DC, 0, x);
+  if (ns > 1) {
+    auto ml_of = [&](int k) { return *reinterpret_cast<const f32x2*>(a.ml_part + paged_part_row(a, at, k) * 2); };
+    float m = kLowest, l = 0.f;
+    for (int k = 0; k < ns; ++k) m = fmaxf(m, ml_of(k)[0]);
+    for (int k = 0; k < ns; ++k) {
+      const f32x2 ml = ml_of(k);
+      l += fast_exp2(ml[0] - m) * ml[1];
+    }
+    const float il = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing: zeros)
+    const float f0 = fast_exp2(ml_of(0)[0] - m) * il;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) x[ks] *= f0;
+    for (int k = 1; k < ns; ++k) {
+      const float* p = a.o_part + paged_part_row(a, at, k) * DC;
+      const float f = fast_exp2(ml_of(k)[0] - m) * il;
+#pragma unroll
+      for (int k0 = 0; k0 < KS; k0 += YS) {
+        f32x8 y[YS];
+        load(p, k0, y);
+#pragma unroll
+        for (int ks = 0; ks < YS; ++ks) x[k0 + ks] += f * y[ks];
+      }
+    }
+  }
+  bf16x8 o[2][KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) two_terms(x[ks], o[0][ks], o[1][ks]);
+
+  for (int v0 = 0; v0 < a.d_v; v0 += VR) {
+    if (v0 > 0) __syncthreads();  // the previous rows are used
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = tid + 256 * i;
+      *reinterpret_cast<u32x4*>(&wl[e / CPR * LS + e % CPR * 8]) = wv[i];
+    }
+    __syncthreads();
+    if (v0 + VR < a.d_v) load_w(v0 + VR);
+#pragma unroll 1
+    for (int vb = 0; vb < VR / 16 && v0 + vb * 16 < a.d_v; ++vb) {
+      f32x4 acc = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 w = as_bf16x8(*reinterpret_cast<const u32x4*>(&wl[(vb * 16 + l16) * LS + ks * 32 + 8 * gq]));
+        acc = mfma16(w, o[0][ks], acc);
+        acc = mfma16(w, o[1][ks], acc);
+      }
+      if (ns > 0) *reinterpret_cast<bf16x4*>(a.out + row * a.d_v + v0 + vb * 16 + 4 * gq) = to_bf16x4(acc);
     }
   }
 }
@@ -644,7 +649,7 @@ void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, in
   }
   *rows = max_rows <= 16 || most == 16 ? 16 : max_rows <= 32 ? 32 : most;
   *unit = 32 * few_waves(d_c);
-  *cost = 1;
+  *cost = 3;
 }
 
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
@@ -666,15 +671,14 @@ hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
 
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s) {
   const int n = a.pg.n_tokens;
-  auto go = [&](auto kernel, int tg) {
-    hipLaunchKernelGGL(kernel, dim3((n + tg - 1) / tg, a.n_heads), dim3(256), 0, s, a);
-    return hipGetLastError();
-  };
-#define X(DC, DR)                                                       \
-  if (a.d_c == DC && a.d_rope == DR) {                                  \
-    if (n <= 128) return go(paged_out_kernel<DC, 1>, 1);                \
-    if (n <= 1024 || DC > 256) return go(paged_out_kernel<DC, 16>, 16); \
-    return go(paged_out_kernel<DC, (DC > 256 ? 16 : 64)>, 64);            \
+#define X(DC, DR)                                                                                        \
+  if (a.d_c == DC && a.d_rope == DR) {                                                                   \
+    if (n <= 128)                                                                                        \
+      hipLaunchKernelGGL(paged_out_row_kernel<DC>, dim3((unsigned)(n * a.n_heads)), dim3(256), 0, s, a);              \
+    else                                                                                                 \
+      hipLaunchKernelGGL(paged_out_tiles_kernel<DC>, dim3((unsigned)(((int64_t)n + 63) / 64 * a.n_heads)), \
+                         dim3(256), 0, s, a);                                                            \
+    return hipGetLastError();                                                                            \
   }
   VMLA_PAGED_SHAPES(X)
 #undef X

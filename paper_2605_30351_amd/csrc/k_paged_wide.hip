@@ -10,7 +10,8 @@
 // scores of 16 keys and its mask is two comparisons with what that row sees, taken only in tiles that
 // cross a row's limits, a hole or the sequence's end. In tiles that cross the limits of the block's rows
 // the workgroup also clears infinities and NaN from the latents between the tile's scores and its PV: a
-// key hidden from a row has probability 0 there, and 0 * NaN would reach it.
+// key hidden from a row has probability 0 there, and 0 * NaN would reach it. The same holds for missing
+// keys (holes, keys past the end), in whose place the pool's first row is staged.
 #include <type_traits>
 
 #include "vmla_paged.h"
@@ -52,14 +53,18 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const PagedWork wk = paged_read<true>(a.plan.work, blockIdx.x);
   int left = wk.n, blk = wk.block, end = wk.end;
 
-  // this wave's loads j = wave + NW i of a tile: in bits 0..15 the offset of this lane's chunk in its row's
-  // c_kv, or (bit 31) k_r (the pad reads k_r again, against zeros in q_cat), in bits 16..20 the tile row
-  uint32_t d_at[C::PER_WAVE];
+  // this wave's loads j = wave + NW i of a tile: where this lane's chunk is in pool row 0 of c_kv, or of k_r
+  // (the pad reads k_r again, against zeros in q_cat); the tile row, and the bytes of a pool row
+  const uint16_t* d_src[C::PER_WAVE];
+  int d_row[C::PER_WAVE];
+  bool d_kr[C::PER_WAVE];
 #pragma unroll
   for (int i = 0; i < C::PER_WAVE; ++i) {
     const int j = wave + NW * i, slot = (j < C::NDMA ? j : 0) * 64 + lane;
     const int r = slot / C::CPR, c = C::pos(r, slot % C::CPR);
-    d_at[i] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : 0x80000000u | (c < (DC + DR) / 8 ? c * 8 - DC : 0));
+    d_row[i] = r;
+    d_kr[i] = c >= DC / 8;
+    d_src[i] = c < DC / 8 ? a.c_kv + c * 8 : a.k_r + (c < (DC + DR) / 8 ? c * 8 - DC : 0);
   }
   // K operand of step ks: row l32, chunk 2 ks + g; V^T transpose reads: rows 4 g + tr_row (+ 8), columns
   // tr_col (+ 32 d, + 16 rows per half)
@@ -70,7 +75,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const int vofs_lo = C::at(4 * g + tr_row, tr_col), vofs_hi = C::at(4 * g + tr_row + 8, tr_col);
 
   while (left > 0) {
-    const PagedBlock pb = paged_read<true>(a.plan.block, blk);
+    const bool last = blk == wk.block;  // (whose record the plan has copied: one load less in line)
+    const PagedBlock pb = last ? paged_read<true>(a.plan.work_block, blockIdx.x) : paged_read<true>(a.plan.block, blk);
     if (end < 0) end = pb.n_units + a.cost;  // a block before the workgroup's last is taken to its end
     const int len = min(left, end), u1 = end - a.cost, u0 = max(u1 - len, 0), n_tiles = u1 - u0;
     left -= len;
@@ -84,23 +90,27 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
 
     // page ids of tile t's keys, one per lane (a key outside the sequence reads the nearest entry)
     auto load_id = [&](int t) { return table[page_of(pg, min(key0 + t * 32 + l32, pg.max_kv - 1))]; };
+    const int key_end = min(key0 + n_tiles * 32, pb.kv);
     auto row_of = [&](int t, int32_t page) {  // this lane's key's pool row, -1: none, or past the segment
       const int key = key0 + t * 32 + l32;
-      if (t >= n_tiles || key >= pb.kv || page < 0 || page >= pg.n_pages) return -1;
-      return page * pg.page_tokens + key - page_of(pg, key) * pg.page_tokens;
+      const int row = page * pg.page_tokens + key - page_of(pg, key) * pg.page_tokens;
+      return key < key_end && (uint32_t)page < (uint32_t)pg.n_pages ? row : -1;
+    };
+    uint32_t from[C::PER_WAVE];  // the pool rows of this lane's chunks (a missing key stages the first row)
+    auto rows_for = [&](int row) {
+#pragma unroll
+      for (int i = 0; i < C::PER_WAVE; ++i) from[i] = __shfl(max(row, 0), d_row[i]);
+    };
+    auto load_part = [&](int i, uint16_t* buf) {
+      const int j = wave + NW * i;
+      if (C::NDMA % NW == 0 || j < C::NDMA)
+        lds_dma16(d_src[i] + (uint64_t)from[i] * (uint32_t)(d_kr[i] ? DR : DC),
+                  __builtin_amdgcn_readfirstlane(lds_addr(buf) + 1024u * j));
     };
     auto load_tile = [&](int row, uint16_t* buf) {
-      const uint32_t lds = lds_addr(buf);
+      rows_for(row);
 #pragma unroll
-      for (int i = 0; i < C::PER_WAVE; ++i) {
-        const int j = wave + NW * i;
-        const int32_t r = __shfl(row, (int)(d_at[i] >> 16) & 31);
-        const bool kr = (int32_t)d_at[i] < 0;
-        const uint16_t* p = kr ? a.k_r : a.c_kv;
-        p += (int64_t)r * (kr ? DR : DC) + (d_at[i] & 0xffffu);
-        if (C::NDMA % NW == 0 || j < C::NDMA)
-          lds_dma16(r < 0 ? a.zero_row : p, __builtin_amdgcn_readfirstlane(lds + 1024u * j));
-      }
+      for (int i = 0; i < C::PER_WAVE; ++i) load_part(i, buf);
     };
     auto exist = [](int row) { return (uint32_t)__builtin_amdgcn_ballot_w64(row >= 0); };
 
@@ -133,9 +143,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     const int e_min = __builtin_amdgcn_readfirstlane(see_e);
     // the latents of tile t in buf, made finite if some row of the block does not see one of its keys
     // (called by all waves, after every wave has used the tile's K and before any uses its V)
-    auto settle = [&](int t, uint16_t* buf) {
+    auto settle = [&](int t, uint32_t keys, uint16_t* buf) {
       const int k0 = key0 + t * 32;
-      if (k0 >= pb.all_b && k0 + 32 <= pb.all_e) return;
+      if (keys == 0xffffffffu && k0 >= pb.all_b && k0 + 32 <= pb.all_e) return;
       for (int i = threadIdx.x; i < 32 * C::CPR; i += NW * 64) {
         u32x4* p = reinterpret_cast<u32x4*>(buf + i * 8);
         *p = as_u32x4(finite_or_zero(as_bf16x8(*p)));
@@ -150,12 +160,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
 
     auto masked_tile = [&](uint32_t keys, int k0) { return keys != 0xffffffffu || k0 < b_max || k0 + 32 > e_min; };
     auto mask = [&](f32x16& s, uint32_t keys, int k0) {
+      const uint32_t seen = seen_keys(keys, see_b - k0, see_e - k0) >> (4 * g);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int k = 8 * (r >> 2) + 4 * g + (r & 3);
-        const bool seen = (keys >> k & 1) && k0 + k >= see_b && k0 + k < see_e;
-        s[r] = seen ? s[r] : kMasked;
-      }
+      for (int r = 0; r < 16; ++r) s[r] = seen >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : kMasked;
     };
     auto max_of = [&](const f32x16& v) {  // a tree of three-input maxima
       const float a0 = fmaxf(fmaxf(v[0], v[1]), v[2]), a1 = fmaxf(fmaxf(v[3], v[4]), v[5]);
@@ -191,12 +198,14 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     // as one fenced stream of slots, K reads two slots and V reads one slot ahead (see k_attend.hip).
     auto step = [&](int t, const f32x16& s_cur, f32x16& s_nxt, const uint16_t* cur, uint16_t* nxt,
                     uint16_t* stg) {
+      // the loads of tile t + 2 go out between the first matrix steps, so that these wait neither for the
+      // exchange of its rows nor for the addresses
       row = row_of(t + 2, id);
-      id = load_id(t + 3);
-      load_tile(row, stg);
+      rows_for(row);
       constexpr int NS = C::KS, NPV = 2 * C::DVB;
       constexpr int NSLOT = NS > NPV + 2 ? NS : NPV + 2;
       constexpr int NSM = NS < 4 ? NS : 4;
+      static_assert(C::PER_WAVE + 1 < NSLOT, "slots for the loads");
       auto kread = [&](int ks) {
         return as_bf16x8(*reinterpret_cast<const u32x4*>(&nxt[((ks & 1) ? koff_o : koff_e) + ks * 16]));
       };
@@ -226,6 +235,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
         if (ks == 0) __builtin_amdgcn_s_setprio(1);
         if (ks == NSLOT / 2) __builtin_amdgcn_s_setprio(0);
         if (ks < NS) acc = mfma32(kq[ks % 3], q[ks], acc);
+        if (ks >= 1 && ks - 1 < C::PER_WAVE) load_part(ks - 1, stg);
+        if (ks == C::PER_WAVE + 1) id = load_id(t + 3);
         if (ks < NSM) {
 #pragma unroll
           for (int p = ks * 8 / NSM; p < (ks + 1) * 8 / NSM; ++p) sm_pair(p);
@@ -242,7 +253,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       there_n = exist(row);
       wait_vmcnt<0>();  // this wave's part of tile t + 2 is in LDS
       __syncthreads();
-      settle(t + 1, nxt);
+      settle(t + 1, keys, nxt);
       if (masked_tile(keys, key0 + (t + 1) * 32)) mask(s_nxt, keys, key0 + (t + 1) * 32);
       own_max = max_of(s_nxt);
       raise_max();
@@ -252,16 +263,18 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     __syncthreads();
     if (row0 >= n_rows) {  // no rows: this wave only loads
       __syncthreads();
-      settle(0, tile[0]);
+      settle(0, there, tile[0]);
       int fill = 2;
       for (int t = 0; t < n_tiles; ++t) {
         row = row_of(t + 2, id);
         id = load_id(t + 3);
         load_tile(row, tile[fill]);
         fill = fill == 2 ? 0 : fill + 1;
+        const uint32_t keys = there_n;
+        there_n = exist(row);
         wait_vmcnt<0>();
         __syncthreads();
-        settle(t + 1, tile[(t + 1) % 3]);
+        settle(t + 1, keys, tile[(t + 1) % 3]);
       }
     } else {
       f32x16 s_a = {}, s_b;
@@ -270,7 +283,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
         s_a = mfma32(as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[0][((ks & 1) ? koff_o : koff_e) + ks * 16])),
                      q[ks], s_a);
       __syncthreads();  // every wave has used tile 0's K
-      settle(0, tile[0]);
+      settle(0, there, tile[0]);
       if (masked_tile(there, key0)) mask(s_a, there, key0);
       own_max = max_of(s_a);
       m_run = fmaxf(kLowest, half_swap_max(own_max));  // nothing to rescale yet
@@ -302,6 +315,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
               *reinterpret_cast<f32x4*>(dst + c) =
                   f32x4{o[d][4 * i] * f, o[d][4 * i + 1] * f, o[d][4 * i + 2] * f, o[d][4 * i + 3] * f};
           }
+        if (u0 == 0 && g == 0)
+          a.plan.row[(int64_t)pb.lo * H + r_own] =
+              PagedRow{(int32_t)blockIdx.x, (uint16_t)(last ? wk.last_ns : 1), (uint16_t)(wave * 32 + l32)};
         if (!whole && g == 0) {
           a.ml_part[prow * 2] = m_run;
           a.ml_part[prow * 2 + 1] = l;

@@ -1064,10 +1064,10 @@ PagedGeo make_paged_geo(const videomla_dims* d, const videomla_paged* p) {
   return g;
 }
 
-// Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots, the
-// plan and the row of zeros.
+// Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots and
+// the plan.
 struct PagedLayout {
-  size_t qcat, o_lat, o_part, ml, zero, head, seq_block, block, first, work, total;
+  size_t qcat, o_lat, o_part, ml, row, block, first, work, work_block, total;
   int32_t rows, unit, cost, max_blocks, n_wg;
 };
 
@@ -1098,12 +1098,11 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
   L.o_lat = take((size_t)rows * d->d_c * 4);
   L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
   L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);
-  L.zero = take(qk * 2);
-  L.head = take(2 * sizeof(int64_t));
-  L.seq_block = take(((size_t)p->n_seqs + 1) * sizeof(int32_t));
+  L.row = take((size_t)rows * sizeof(PagedRow));
   L.block = take((size_t)L.max_blocks * sizeof(PagedBlock));
-  L.first = take(((size_t)L.max_blocks + 1) * sizeof(int64_t));
+  L.first = take((size_t)L.max_blocks * sizeof(int64_t));
   L.work = take((size_t)L.n_wg * sizeof(PagedWork));
+  L.work_block = take((size_t)L.n_wg * sizeof(PagedBlock));
   L.total = at;
   return L;
 }
@@ -1162,12 +1161,11 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   a.o_lat = reinterpret_cast<float*>(ws + L.o_lat);
   a.o_part = reinterpret_cast<float*>(ws + L.o_part);
   a.ml_part = reinterpret_cast<float*>(ws + L.ml);
-  a.zero_row = reinterpret_cast<uint16_t*>(ws + L.zero);
-  a.plan.head = reinterpret_cast<int64_t*>(ws + L.head);
-  a.plan.seq_block = reinterpret_cast<int32_t*>(ws + L.seq_block);
+  a.plan.row = reinterpret_cast<PagedRow*>(ws + L.row);
   a.plan.block = reinterpret_cast<PagedBlock*>(ws + L.block);
   a.plan.first = reinterpret_cast<int64_t*>(ws + L.first);
   a.plan.work = reinterpret_cast<PagedWork*>(ws + L.work);
+  a.plan.work_block = reinterpret_cast<PagedBlock*>(ws + L.work_block);
   a.max_blocks = L.max_blocks; a.rows = L.rows; a.unit = L.unit; a.cost = L.cost;
   a.batch = 1; a.n_heads = d->n_heads; a.d_nope = d->d_nope; a.d_rope = d->d_rope;
   a.d_c = d->d_c; a.d_v = d->d_v;

@@ -50,7 +50,7 @@ struct PagedSeq {
 // scalar load, which does not wait for the vector loads in flight.
 template <bool UNIFORM, class T>
 __device__ __forceinline__ T paged_read(const T* p, int64_t i) {
-  if constexpr (UNIFORM && sizeof(T) > 8) {
+  if constexpr (UNIFORM && !std::is_integral<T>::value) {
     typedef uint32_t words __attribute__((ext_vector_type(sizeof(T) / 4)));
     typedef const __attribute__((address_space(4))) words* scalar_ptr;
     return __builtin_bit_cast(T, *(scalar_ptr)(uintptr_t)(p + i));
@@ -73,19 +73,9 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedGeo& g, int s) {
   return q;
 }
 
-// The sequence of token row t (cu[s] <= t < cu[s + 1]), or -1 behind the last one.
-__device__ __forceinline__ int paged_seq_of(const PagedGeo& g, int t) {
-  int lo = 0, hi = g.n_seqs;  // the first s with cu[s + 1] > t
-  while (lo < hi) {
-    const int m = (lo + hi) >> 1;
-    if (g.cu[m + 1] > t) hi = m;
-    else lo = m + 1;
-  }
-  return lo < g.n_seqs && t >= g.cu[lo] ? lo : -1;
-}
-
-// The same for a token row per lane (all lanes of the wave take part): the first 64 steps of the search
-// come from one load, a lane each, and the rest, for more than 64 sequences, from memory.
+// The sequence of token row t (cu[s] <= t < cu[s + 1]), or -1 behind the last one, for a row per lane (all
+// lanes of the wave take part): the ends of 64 groups of sequences come from one load, a lane each, and
+// the rest of the search, for more than 64 sequences, from memory.
 __device__ __forceinline__ int paged_seq_of_lanes(const PagedGeo& g, int t) {
   const int lane = threadIdx.x & 63, stride = (g.n_seqs + 63) >> 6;
   const int end = g.cu[min((lane + 1) * stride, g.n_seqs)];  // end of the lane's group of sequences
@@ -105,14 +95,6 @@ __device__ __forceinline__ int paged_seq_of_lanes(const PagedGeo& g, int t) {
     }
   }
   return lo < g.n_seqs && t >= g.cu[lo] ? lo : -1;
-}
-
-// The pool row of cached token j, -1 for a hole (j outside the sequence, or its page outside the pool).
-__device__ __forceinline__ int32_t paged_row(const PagedGeo& g, int s, int32_t kv, int32_t j) {
-  if (j < 0 || j >= kv) return -1;
-  const int32_t p = page_of(g, j);
-  const int32_t page = g.table[(int64_t)s * g.max_pages + p];
-  return page < 0 || page >= g.n_pages ? -1 : page * g.page_tokens + (j - p * g.page_tokens);
 }
 
 // (f, y, x) of an absolute position.
@@ -147,6 +129,12 @@ __device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q,
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kMasked = -__builtin_huge_valf();
 constexpr float kLazyMaxStep = 8.0f;  // the running max is raised when exceeded by more (log2 units)
+
+// Of 32 keys, those of the bit set `keys` in [b, e).
+__device__ __forceinline__ uint32_t seen_keys(uint32_t keys, int b, int e) {
+  const int lo = min(max(b, 0), 32), hi = min(max(e, 0), 32);
+  return keys & (uint32_t)(((uint64_t)1 << hi) - ((uint64_t)1 << min(lo, hi)));
+}
 
 // bf16 values with infinities and NaN replaced by zero. In a tile that is masked for some row, a key's
 // probability may be 0 while its latent is not finite, and 0 * NaN would reach the rows that do not see
@@ -200,14 +188,27 @@ __device__ __forceinline__ void paged_row_sees(const PagedGeo& g, const PagedBlo
 }
 
 struct PagedWork {
-  int32_t block, end, n, pad;  // last row block, the end in its counts, counts of the workgroup
+  int32_t block, end, n, last_ns;  // last row block, the end in its counts, counts of the workgroup; the
+                                   // workgroups that share the last block
 };
+// Where a row's latents are, written by the workgroup that has its block's first unit (the absorb kernel
+// clears it): ns workgroups share its block, w0 the first of them, row its place in the block; ns 1: its
+// row of o_lat; ns 0: the row belongs to no sequence.
+struct PagedRow {
+  int32_t w0;
+  uint16_t ns, row;
+};
+// The workgroup that takes count u of U, split over G.
+__device__ __forceinline__ int paged_owner(int64_t u, int64_t U, int64_t G) {
+  return (int)floor_div((u + 1) * G - 1, U);
+}
+
 struct PagedPlan {
-  int64_t* head;        // [2]: counts U, workgroups G in use
-  int32_t* seq_block;   // [n_seqs + 1] first row block of each sequence
-  PagedBlock* block;    // [max_blocks]
-  int64_t* first;       // [max_blocks + 1] first count of each block
-  PagedWork* work;      // [n_wg]
+  int64_t* first;         // [max_blocks] first count of each block
+  PagedBlock* block;      // [max_blocks]
+  PagedWork* work;        // [n_wg]
+  PagedBlock* work_block; // [n_wg] the record of work[].block
+  PagedRow* row;          // [n_tokens * H]
 };
 
 struct PagedWriteArgs : WriteArgs {
@@ -218,7 +219,6 @@ struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
   float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
-  uint16_t* zero_row;  // workspace: a row of zeros, staged in a hole's place
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
   int32_t cost;        // counts of a block beyond its units
@@ -228,6 +228,7 @@ constexpr int kPagedMaxSeqs = 4096;
 
 hipError_t launch_paged_cache_write(const PagedWriteArgs& a, hipStream_t s);
 hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s);
+hipError_t launch_paged_absorb_tiles(const PagedAttendArgs& a, hipStream_t s);  // (k_attend.hip)
 hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s);
 

@@ -7,10 +7,10 @@ namespace vmla {
 // By one workgroup of 256 threads, beside the workgroups that absorb the queries: its chain of loads and
 // scans, 6 to 8 us, then passes under theirs (a launch of its own took that long and stood in line).
 constexpr int kPlanThreads = 256;
+constexpr int kPlanNear = 512;  // blocks whose first counts are searched in LDS
 
 // Exclusive prefix sums of v over the workgroup's threads; total: the sum.
-__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t& total) {
-  __shared__ int64_t wave_sum[kPlanThreads / 64];
+__device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t& total, int64_t* wave_sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t x = v;
 #pragma unroll
@@ -30,8 +30,13 @@ __device__ __forceinline__ int64_t plan_scan(int64_t v, int64_t& total) {
   return base + x - v;
 }
 
-__device__ __forceinline__ void paged_plan(const PagedAttendArgs& a) {
-  __shared__ int32_t first_block[kPagedMaxSeqs + 1];
+// lds: kPlanLds bytes, the other workgroups' staging area (an array of its own would cost all of them).
+constexpr int kPlanLds = kPlanNear * 8 + kPlanThreads / 64 * 8 + (kPagedMaxSeqs + 2) * 4;
+
+__device__ __forceinline__ void paged_plan(const PagedAttendArgs& a, void* lds) {
+  int64_t* const first_near = reinterpret_cast<int64_t*>(lds);
+  int64_t* const wave_sum = first_near + kPlanNear;
+  int32_t* const first_block = reinterpret_cast<int32_t*>(wave_sum + kPlanThreads / 64);
   const PagedGeo& g = a.pg;
   const int tid = (int)threadIdx.x, H = a.n_heads, R = a.rows;
   int64_t blocks = 0;
@@ -42,7 +47,7 @@ __device__ __forceinline__ void paged_plan(const PagedAttendArgs& a) {
       const PagedSeq q = paged_seq(g, s);
       n = ((int64_t)(q.hi - q.lo) * H + R - 1) / R;
     }
-    const int64_t at = blocks + plan_scan(n, total);
+    const int64_t at = blocks + plan_scan(n, total, wave_sum);
     // offsets that go down could ask for more blocks than the call's rows make: those are left out
     if (s < g.n_seqs) first_block[s] = (int32_t)min(at, (int64_t)a.max_blocks);
     blocks += total;
@@ -50,7 +55,6 @@ __device__ __forceinline__ void paged_plan(const PagedAttendArgs& a) {
   blocks = min(blocks, (int64_t)a.max_blocks);
   if (tid == 0) first_block[g.n_seqs] = (int32_t)blocks;
   __syncthreads();
-  for (int s = tid; s <= g.n_seqs; s += kPlanThreads) a.plan.seq_block[s] = first_block[s];
   int64_t units = 0;
   for (int r0 = 0; r0 < blocks; r0 += kPlanThreads) {
     const int r = r0 + tid;
@@ -85,17 +89,16 @@ __device__ __forceinline__ void paged_plan(const PagedAttendArgs& a) {
       a.plan.block[r] = p;
       n = p.n_units + a.cost;
     }
-    const int64_t at = units + plan_scan(n, total);
-    if (r < blocks) a.plan.first[r] = at;
+    const int64_t at = units + plan_scan(n, total, wave_sum);
+    if (r < blocks) {
+      a.plan.first[r] = at;
+      if (r < kPlanNear) first_near[r] = at;
+    }
     units += total;
-  }
-  if (tid == 0) {
-    a.plan.first[blocks] = units;
-    a.plan.head[0] = units;
-    a.plan.head[1] = min(units, (int64_t)a.n_wg);
   }
   __syncthreads();
   const int64_t G = min(units, (int64_t)a.n_wg);
+  auto first_of = [&](int b) { return b < kPlanNear ? first_near[b] : a.plan.first[b]; };
   for (int w = tid; w < a.n_wg; w += kPlanThreads) {
     PagedWork k{};
     if (w < G) {
@@ -103,17 +106,19 @@ __device__ __forceinline__ void paged_plan(const PagedAttendArgs& a) {
       int lo = 0, hi = (int)blocks - 1;  // the last block with first < u1
       while (lo < hi) {
         const int m = (lo + hi + 1) >> 1;
-        if (a.plan.first[m] < u1) lo = m;
+        if (first_of(m) < u1) lo = m;
         else hi = m - 1;
       }
       k.block = lo;
-      k.end = (int32_t)(u1 - a.plan.first[lo]);
+      const int64_t at = first_of(lo);
+      const PagedBlock p = a.plan.block[lo];
+      k.end = (int32_t)(u1 - at);
       k.n = (int32_t)(u1 - u);
+      k.last_ns = paged_owner(at + a.cost + p.n_units - 1, units, G) - paged_owner(at + a.cost, units, G) + 1;
+      a.plan.work_block[w] = p;
     }
     a.plan.work[w] = k;
   }
-  // the row that is staged in place of a hole
-  for (int i = tid; i < a.dqk_pad; i += kPlanThreads) a.zero_row[i] = 0;
 }
 
 }  // namespace vmla
