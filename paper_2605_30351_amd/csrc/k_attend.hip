@@ -174,6 +174,9 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
             const f32x4 v = {acc[cb][4 * i] * a.qscale, acc[cb][4 * i + 1] * a.qscale,
                              acc[cb][4 * i + 2] * a.qscale, acc[cb][4 * i + 3] * a.qscale};
             *reinterpret_cast<bf16x4*>(STAGE ? ot + l32 * OS + c : dst + c) = to_bf16x4(v);
+            if constexpr (PAGED) {
+              if (ok) paged_q_lo(a, (int64_t)row * DQKP + c, v);
+            }
           }
         }
     }
@@ -186,6 +189,9 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
     const size_t r = ((size_t)b * Nq + t) * H + h;
     float u = bf16_bits_to_f32((uint16_t)(raw & 0xffff)), v = bf16_bits_to_f32((uint16_t)(raw >> 16));
     rotate_by(rope_cos_sin_at(qpos[wave][rp.axis][t - tok0], rp.theta), u, v);
+    if constexpr (PAGED) {
+      if (a.q_lo) paged_q_pair(a, (int64_t)r * DQKP + DC + 2 * p, u * a.qscale, v * a.qscale);
+    }
     const uint32_t packed =
         (uint32_t)to_bf16_bits(u * a.qscale) | ((uint32_t)to_bf16_bits(v * a.qscale) << 16);
     *reinterpret_cast<uint32_t*>(STAGE ? ot + (t - tok0) * OS + DC + 2 * p
@@ -214,6 +220,9 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
       for (int c = DC + DR; c < DQKP; ++c) {
         if (STAGE) ot[(t - tok0) * OS + c] = 0;
         else a.qcat[r * DQKP + c] = 0;
+        if constexpr (PAGED) {
+          if (a.q_lo) a.q_lo[r * DQKP + c] = 0;
+        }
       }
     }
   }

@@ -16,12 +16,6 @@
 namespace vmla {
 namespace {
 
-// D(16x16) += A(16x32) B(32x16). Lane l holds A[l%16][8(l/16) .. +8], B[8(l/16) .. +8][l%16];
-// accumulator element i of lane l is D[4(l/16) + i][l%16].
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-
 typedef __attribute__((address_space(3))) int32_t lds_i32;
 
 // Direct global-to-LDS load of 4 B per lane: lane l's word lands at lds_base + 4 l (see lds_dma16).
@@ -32,14 +26,6 @@ __device__ __forceinline__ void lds_dma4(const int32_t* gptr, uint32_t lds_base)
                : "memory", "m0");
 }
 
-// The same of 16 B from a scalar base and a lane offset in bytes. The base has to be settled (no VALU
-// instruction may write it in the five wait states before): callers compute it with scalar arithmetic.
-__device__ __forceinline__ void lds_dma16_row(const void* base, uint32_t off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(off), "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
 // Waits until at most N vector-memory operations of the wave are outstanding; later LDS reads stay behind.
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -63,15 +49,16 @@ struct FewCfg {
   static constexpr int NDMA = 32 * CPR / 64;             // 1 KB loads per tile
   static constexpr int NW = few_waves(DC);
   static constexpr int ROWS = 16 * QB;
-  static constexpr int QP = QB % 2 ? 1 : 2;              // 16-row blocks merged at a time
   static constexpr int UNIT = 32 * NW;
   static constexpr int RS = DC + 4;                      // row stride of the merged latents (floats)
   // Tile layout. d_c = 512: c_kv rows of 1 KB, so that a load is one row from a scalar base, then the k_r
   // rows. Otherwise rows [c_kv | k_r | pad].
   static constexpr bool SPLIT = DC == 512;
   static constexpr int STRIDE = SPLIT ? DC : DQKP;
-  // The queries are in LDS where with the accumulators they would fill the registers.
-  static constexpr bool QLDS = QB * (KS + DV) * 4 > 190;
+  // The absorbed queries' two bf16 terms (see the scores). They are in LDS where with the accumulators they
+  // would fill the registers: both, or at d_c = 512, where the tiles leave no room for more, the first.
+  static constexpr bool QLDS = QB * (2 * KS + DV) * 4 > 190;
+  static constexpr bool LO_REG = !QLDS || SPLIT;
   // Chunk position of logical chunk c in row r. CPR is 4 or 12 mod 16, so the rows r .. r + 3 of one
   // chunk fall on different groups of four 4-bank groups; the XOR separates the rows 4 apart, by bit 1
   // first, since the transpose reads take two adjacent chunks of rows 4 j .. 4 j + 3 and the next four.
@@ -84,7 +71,7 @@ struct FewCfg {
   __device__ static constexpr int swz16(int r) { return ((r << 1) & 15) | ((r >> 3) & 1); }
   static_assert(CPR % 16 == 4 || CPR % 16 == 12, "bank spread of the tile rows");
   static_assert(DC % 16 == 0 && 16 * CPR % 64 == 0 && NDMA + 1 < 64, "tile shape");
-  static_assert(16 * QP * RS * 4 <= 2 * TILE * 2, "a wave's results fit its tile buffers");
+  static_assert(ROWS * RS * 4 <= 2 * TILE * 2, "a wave's results fit its tile buffers");
 };
 
 template <int DC, int DR, int QB>
@@ -92,9 +79,9 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
   using C = FewCfg<DC, DR, QB>;
   constexpr int NW = C::NW;
   __shared__ __attribute__((aligned(16))) uint16_t tiles[NW][2][C::TILE];
-  __shared__ __attribute__((aligned(16))) uint16_t qs[C::QLDS ? C::ROWS * C::DQKP : 8];
+  __shared__ __attribute__((aligned(16))) uint16_t qs[C::QLDS ? (C::LO_REG ? 1 : 2) * C::ROWS * C::DQKP : 8];
   __shared__ int32_t ids[NW][2][64];
-  __shared__ float red_m[NW][16 * C::QP], red_l[NW][16 * C::QP];
+  __shared__ float red_m[NW][C::ROWS], red_l[NW][C::ROWS];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -144,7 +131,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
     load_ids(1);
 
     // this lane's rows and what they see
-    bf16x8 qv[C::QLDS ? 1 : QB][C::KS];
+    bf16x8 qv[C::QLDS ? 1 : QB][C::KS], qlo[C::LO_REG ? QB : 1][C::KS];
     int see_b[QB], see_e[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -152,25 +139,29 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       see_b[qb] = 0;
       see_e[qb] = 0x7fffffff;
       if (r < n_rows) paged_row_sees(g, pb, H, 16 * qb + l16, see_b[qb], see_e[qb]);
-      if constexpr (!C::QLDS) {
-        const uint16_t* src = a.qcat + ((int64_t)pb.lo * H + (r < n_rows ? r : row0)) * C::DQKP + 8 * gq;
+      auto own_row = [&](const uint16_t* q, bf16x8 (&v)[C::KS]) {
+        const uint16_t* src = q + ((int64_t)pb.lo * H + (r < n_rows ? r : row0)) * C::DQKP + 8 * gq;
 #pragma unroll
         for (int ks = 0; ks < C::KS; ++ks) {
-          u32x4 v = ldg16(src + ks * 32);
-          if (r >= n_rows) v = u32x4{0, 0, 0, 0};
-          qv[qb][ks] = as_bf16x8(v);
+          u32x4 x = ldg16(src + ks * 32);
+          if (r >= n_rows) x = u32x4{0, 0, 0, 0};
+          v[ks] = as_bf16x8(x);
         }
-      }
+      };
+      if constexpr (!C::QLDS) own_row(a.qcat, qv[qb]);
+      if constexpr (C::LO_REG) own_row(a.q_lo, qlo[qb]);
     }
     if constexpr (C::QLDS) {  // laid out as the tile's rows, so that the reads are as free of conflicts
-      for (int i = threadIdx.x; i < C::ROWS * C::CPR; i += NW * 64) {
-        const int r = i / C::CPR, c = i % C::CPR;
-        u32x4 v = ldg16(a.qcat + ((int64_t)pb.lo * H + row0 + (row0 + r < n_rows ? r : 0)) * C::DQKP + c * 8);
+      for (int i = threadIdx.x; i < (C::LO_REG ? 1 : 2) * C::ROWS * C::CPR; i += NW * 64) {
+        const int rr = i / C::CPR, c = i % C::CPR, r = rr % C::ROWS;
+        u32x4 v = ldg16((rr < C::ROWS ? a.qcat : a.q_lo) +
+                        ((int64_t)pb.lo * H + row0 + (row0 + r < n_rows ? r : 0)) * C::DQKP + c * 8);
         if (row0 + r >= n_rows) v = u32x4{0, 0, 0, 0};
-        *reinterpret_cast<u32x4*>(&qs[r * C::DQKP + (c ^ C::swz(r)) * 8]) = v;
+        *reinterpret_cast<u32x4*>(&qs[rr * C::DQKP + (c ^ C::swz(r)) * 8]) = v;
       }
       __syncthreads();
     }
+
     f32x4 o[QB][C::DV];
     float m_run[QB], l_run[QB];
 #pragma unroll
@@ -192,10 +183,12 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       const int at_row = max(row, 0);  // in a missing key's place, the pool's first row: masked, made finite
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_addr(&tiles[wave][t & 1][0]));
       if constexpr (C::SPLIT) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));  // the 16 offsets are recomputed: kept across the loop they would spill
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           const uint32_t r = __builtin_amdgcn_readlane(at_row, j);
-          lds_dma16_row(a.c_kv + (uint64_t)r * DC, (lane ^ C::swz16(j)) * 16, lds + 1024u * j);
+          lds_dma16_row(a.c_kv + (uint64_t)r * DC, (ln ^ C::swz16(j)) * 16, lds + 1024u * j);
         }
       }
 #pragma unroll
@@ -203,7 +196,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
         const int half = C::SPLIT ? j - 32 : j / NAT;
         uint32_t at = d_at[j % NAT];
         // recomputed from one register a load: kept across the loop, the addresses' parts would fill the file
-        if constexpr (QB * DC >= 256) asm volatile("" : "+v"(at));
+        if constexpr (DC == 256) asm volatile("" : "+v"(at));
         const uint32_t r = __shfl(at_row, (int)(at >> 16 & 15) + 16 * half);
         const bool kr = (int32_t)at < 0;
         const uint16_t* p = (kr ? a.k_r : a.c_kv) + (at & 0xffffu);
@@ -238,10 +231,10 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       if constexpr (C::SPLIT) return v_base[d & 7] + (d >> 3) * 128;
       else return v_base[d & 1] + (d >> 1) * 32;
     };
-    auto q_at = [&](int qb, int ks) {
+    auto q_at = [&](int term, int qb, int ks) {
       if constexpr (C::QLDS)
         return as_bf16x8(*reinterpret_cast<const u32x4*>(
-            &qs[(16 * qb + l16) * C::DQKP + ((gq ^ C::swz(l16)) << 3) + ks * 32]));
+            &qs[(term * C::ROWS + 16 * qb + l16) * C::DQKP + ((gq ^ C::swz(l16)) << 3) + ks * 32]));
       else return qv[qb][ks];
     };
 
@@ -250,6 +243,10 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       const uint16_t* tile = tiles[wave][t & 1];
       const bool masked = there != 0xffffffffu || k0 < pb.all_b || k0 + 32 > pb.all_e;
 
+      // Both terms of the absorbed queries: one alone is off by up to 2^-8 of each component, which moves a
+      // score of size |s| by about 2^-9.5 |s| and weighs most where the softmax is peaked (scores of standard
+      // deviation 4: outputs off by 0.0044 in the 2-norm with one term, 0.0025 with two). These matrix steps
+      // pass under the loads of the keys, which bound this kernel.
       f32x4 s[QB][2];
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{};
@@ -259,9 +256,14 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
         const bf16x8 k1v = as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[k_at(1, ks)]));
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-          const bf16x8 qk = q_at(qb, ks);
+          const bf16x8 qk = q_at(0, qb, ks);
           s[qb][0] = mfma16(k0v, qk, s[qb][0]);
           s[qb][1] = mfma16(k1v, qk, s[qb][1]);
+          bf16x8 ql;
+          if constexpr (C::LO_REG) ql = qlo[qb][ks];
+          else ql = q_at(1, qb, ks);
+          s[qb][0] = mfma16(k0v, ql, s[qb][0]);
+          s[qb][1] = mfma16(k1v, ql, s[qb][1]);
         }
       }
       if (masked) {
@@ -347,57 +349,52 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       }
     }
 
-    // ---- the waves' results, merged in wave order, 16 QP rows at a time ----
-    float* res = reinterpret_cast<float*>(&tiles[wave][0][0]);  // [16 QP][RS]: this wave's own buffers
+    // ---- the waves' results, merged in wave order ----
+    float* res = reinterpret_cast<float*>(&tiles[wave][0][0]);  // [ROWS][RS]: this wave's own buffers
     const bool whole = take == pb.n_units;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (u0 == 0);
     if (u0 == 0 && (int)threadIdx.x < C::ROWS && row0 + (int)threadIdx.x < n_rows)
       a.plan.row[(int64_t)pb.lo * H + row0 + threadIdx.x] =
           PagedRow{(int32_t)blockIdx.x, (uint16_t)(last ? wk.last_ns : 1), (uint16_t)threadIdx.x};
 #pragma unroll
-    for (int q0 = 0; q0 < QB; q0 += C::QP) {
-#pragma unroll
-      for (int qp = 0; qp < C::QP; ++qp) {
-        const int qb = q0 + qp;
-        float l = l_run[qb];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (gq == 0) {
-          red_m[wave][16 * qp + l16] = m_run[qb];
-          red_l[wave][16 * qp + l16] = l;
-        }
-#pragma unroll
-        for (int d = 0; d < C::DV; ++d)
-          *reinterpret_cast<f32x4*>(&res[(16 * qp + l16) * C::RS + 16 * d + 4 * gq]) = o[qb][d];
+    for (int qb = 0; qb < QB; ++qb) {
+      float l = l_run[qb];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (gq == 0) {
+        red_m[wave][16 * qb + l16] = m_run[qb];
+        red_l[wave][16 * qb + l16] = l;
       }
-      __syncthreads();
-      for (int i = threadIdx.x; i < 16 * C::QP * (DC / 4); i += NW * 64) {
-        const int rr = i / (DC / 4), r = 16 * q0 + rr, c = i % (DC / 4) * 4;
-        if (row0 + r >= n_rows) break;
-        float m = kLowest, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][rr]);
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const float f = fast_exp2(red_m[w][rr] - m);
-          l += f * red_l[w][rr];
-          v += f * *reinterpret_cast<const f32x4*>(
-                       reinterpret_cast<const float*>(&tiles[w][0][0]) + rr * C::RS + c);
-        }
-        if (whole) {
-          v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-          *reinterpret_cast<f32x4*>(a.o_lat + ((int64_t)pb.lo * H + row0 + r) * DC + c) = v;
-        } else {
-          *reinterpret_cast<f32x4*>(a.o_part + (slot * C::ROWS + r) * DC + c) = v;
-          if (c == 0) {
-            a.ml_part[(slot * C::ROWS + r) * 2] = m;
-            a.ml_part[(slot * C::ROWS + r) * 2 + 1] = l;
-          }
-        }
-      }
-      __syncthreads();  // the buffers are free for the next rows or segment
+      for (int d = 0; d < C::DV; ++d)
+        *reinterpret_cast<f32x4*>(&res[(16 * qb + l16) * C::RS + 16 * d + 4 * gq]) = o[qb][d];
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < C::ROWS * (DC / 4); i += NW * 64) {
+      const int r = i / (DC / 4), c = i % (DC / 4) * 4;
+      if (row0 + r >= n_rows) break;
+      float m = kLowest, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, red_m[w][r]);
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float f = fast_exp2(red_m[w][r] - m);
+        l += f * red_l[w][r];
+        v += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(&tiles[w][0][0]) + r * C::RS + c);
+      }
+      if (whole) {
+        v *= l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
+        *reinterpret_cast<f32x4*>(a.o_lat + ((int64_t)pb.lo * H + row0 + r) * DC + c) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(a.o_part + (slot * C::ROWS + r) * DC + c) = v;
+        if (c == 0) {
+          a.ml_part[(slot * C::ROWS + r) * 2] = m;
+          a.ml_part[(slot * C::ROWS + r) * 2 + 1] = l;
+        }
+      }
+    }
+    __syncthreads();  // the buffers are free for the next block
   }
 }
 
@@ -635,8 +632,10 @@ __global__ __launch_bounds__(256, DC <= 192 ? 4 : DC <= 256 ? 3 : 2) void paged_
 }  // namespace
 
 namespace {
-// 16-row blocks per workgroup of the few-row kernel: the most whose accumulators leave the registers room
-constexpr int few_most(int dc) { return dc <= 128 ? 4 : dc <= 192 ? 3 : 1; }
+// 16-row blocks per workgroup of the few-row kernel, at most: beyond, the wide kernel is as fast or faster. us,
+// few / wide, d_c = 192: 24 rows x 8 sequences of up to 16,000 keys 17.2 / 14.4, up to 32,760 31.2 / 35.0; 48 rows
+// 23.9 / 15.6 and 45.1 / 37.9. At d_c = 256 and 512 two blocks' accumulators and queries do not fit.
+constexpr int few_most(int dc) { return dc <= 192 ? 2 : 1; }
 }  // namespace
 
 void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit, int32_t* cost) {
@@ -647,7 +646,7 @@ void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, in
     *cost = 8;
     return;
   }
-  *rows = max_rows <= 16 || most == 16 ? 16 : max_rows <= 32 ? 32 : most;
+  *rows = max_rows <= 16 ? 16 : most;
   *unit = 32 * few_waves(d_c);
   *cost = 3;
 }
@@ -661,7 +660,6 @@ hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
 #define X(DC, DR)                                                                                     \
   if (a.d_c == DC && a.d_rope == DR) {                                                                \
     if (a.rows == 16) return go(paged_attend_few_kernel<DC, DR, 1>);                                  \
-    if (a.rows == 32) return go(paged_attend_few_kernel<DC, DR, (few_most(DC) > 1 ? 2 : 1)>);         \
     return go(paged_attend_few_kernel<DC, DR, few_most(DC)>);                                         \
   }
   VMLA_PAGED_SHAPES(X)
@@ -669,12 +667,18 @@ hipError_t launch_paged_attend(const PagedAttendArgs& a, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
+// The output kernel by row costs about 3 us and 1 us per 150 rows, whatever the splits; the one by tiles 9 us,
+// 1 us per 1,500 rows and 2.3 us per split, which it merges one after the other (d_c = 192). us, row / tiles:
+// 384 rows x 8 splits 6.2 / 12, 1,536 x 8 14.0 / 31, 1,536 x 32 16.8 / 81, 3,600 x 17 28.9 / 58,
+// 1,440 x 2 12.6 / 12, 33,696 x 2 198 / 24. Splits are estimated from the row blocks that the tensors' sizes allow.
 hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s) {
   const int n = a.pg.n_tokens;
+  const int64_t rows = (int64_t)n * a.n_heads, blocks = rows / a.rows + 1;
+  const bool by_row = rows <= 1000 + 400 * (a.n_wg / blocks);
 #define X(DC, DR)                                                                                        \
   if (a.d_c == DC && a.d_rope == DR) {                                                                   \
-    if (n <= 128)                                                                                        \
-      hipLaunchKernelGGL(paged_out_row_kernel<DC>, dim3((unsigned)(n * a.n_heads)), dim3(256), 0, s, a);              \
+    if (by_row)                                                                                          \
+      hipLaunchKernelGGL(paged_out_row_kernel<DC>, dim3((unsigned)rows), dim3(256), 0, s, a);            \
     else                                                                                                 \
       hipLaunchKernelGGL(paged_out_tiles_kernel<DC>, dim3((unsigned)(((int64_t)n + 63) / 64 * a.n_heads)), \
                          dim3(256), 0, s, a);                                                            \

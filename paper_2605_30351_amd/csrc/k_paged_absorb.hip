@@ -13,6 +13,9 @@ namespace vmla {
 namespace {
 
 constexpr int kFewTokens = 4;
+// Calls of up to this many tokens take this kernel. d_c = 192, 12 heads, us here / matrix kernel: 68 tokens
+// 7.5 / 11.0, 132 tokens 8.6 / 13.2, 244 tokens 10.4 / 13.2; d_c = 512, 132 tokens 13.0 / 29.3.
+constexpr int kFewCalls = 256;
 constexpr int kFewMaxNope = 128;
 
 template <int DC, int DR>
@@ -58,11 +61,10 @@ __global__ __launch_bounds__(256) void paged_absorb_few_kernel(const PagedAttend
       const uint32_t raw = *reinterpret_cast<const uint32_t*>(a.q_r + row * DR + 2 * pr);
       float u = bf16_bits_to_f32((uint16_t)(raw & 0xffff)), v = bf16_bits_to_f32((uint16_t)(raw >> 16));
       rope_rotate(a.rope, pr, pos, u, v);
-      *reinterpret_cast<uint32_t*>(a.qcat + row * DQKP + DC + 2 * pr) =
-          (uint32_t)to_bf16_bits(u * a.qscale) | ((uint32_t)to_bf16_bits(v * a.qscale) << 16);
+      paged_q_pair(a, row * DQKP + DC + 2 * pr, u * a.qscale, v * a.qscale);
       if (pr == 0) {
         a.plan.row[row] = PagedRow{};
-        for (int c = DC + DR; c < DQKP; ++c) a.qcat[row * DQKP + c] = 0;
+        for (int c = DC + DR; c < DQKP; c += 2) paged_q_pair(a, row * DQKP + c, 0.f, 0.f);
       }
     }
   }
@@ -109,14 +111,16 @@ __global__ __launch_bounds__(256) void paged_absorb_few_kernel(const PagedAttend
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int g = 0; g < RG; ++g) v += *reinterpret_cast<const f32x4*>(&red[g][t][c]);
-    *reinterpret_cast<bf16x4*>(a.qcat + ((int64_t)(t0 + t) * H + h) * DQKP + c) = to_bf16x4(v * a.qscale);
+    const int64_t at = ((int64_t)(t0 + t) * H + h) * DQKP + c;
+    *reinterpret_cast<bf16x4*>(a.qcat + at) = to_bf16x4(v * a.qscale);
+    paged_q_lo(a, at, v * a.qscale);
   }
 }
 
 }  // namespace
 
 hipError_t launch_paged_absorb(const PagedAttendArgs& a, hipStream_t s) {
-  if (a.pg.n_tokens > 64) return launch_paged_absorb_tiles(a, s);
+  if (a.pg.n_tokens > kFewCalls) return launch_paged_absorb_tiles(a, s);
   const dim3 grid((a.pg.n_tokens + kFewTokens - 1) / kFewTokens + 1, a.n_heads);
 #define X(DC, DR)                                                                        \
   if (a.d_c == DC && a.d_rope == DR) {                                                   \

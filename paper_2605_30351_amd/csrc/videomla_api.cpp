@@ -1067,7 +1067,7 @@ PagedGeo make_paged_geo(const videomla_dims* d, const videomla_paged* p) {
 // Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots and
 // the plan.
 struct PagedLayout {
-  size_t qcat, o_lat, o_part, ml, row, block, first, work, work_block, total;
+  size_t qcat, q_lo, o_lat, o_part, ml, row, block, first, work, work_block, total;
   int32_t rows, unit, cost, max_blocks, n_wg;
 };
 
@@ -1095,6 +1095,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
     return off;
   };
   L.qcat = take((size_t)rows * qk * 2);
+  L.q_lo = L.unit > 32 ? take((size_t)rows * qk * 2) : 0;  // (the few-row kernel)
   L.o_lat = take((size_t)rows * d->d_c * 4);
   L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
   L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);
@@ -1158,6 +1159,7 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   PagedAttendArgs a{};
   a.q_nope = q_nope; a.q_r = q_r; a.w_uk = w_uk; a.w_uv = w_uv; a.c_kv = c_kv; a.k_r = k_r; a.out = out;
   a.qcat = reinterpret_cast<uint16_t*>(ws + L.qcat);
+  a.q_lo = L.q_lo ? reinterpret_cast<uint16_t*>(ws + L.q_lo) : nullptr;
   a.o_lat = reinterpret_cast<float*>(ws + L.o_lat);
   a.o_part = reinterpret_cast<float*>(ws + L.o_part);
   a.ml_part = reinterpret_cast<float*>(ws + L.ml);

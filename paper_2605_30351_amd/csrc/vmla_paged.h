@@ -124,6 +124,21 @@ __device__ __forceinline__ void paged_seen(const PagedGeo& g, const PagedSeq& q,
   beg = g.window > 0 ? end - g.window : -kPagedFar;
 }
 
+// D(16x16) += A(16x32) B(32x16). Lane l holds A[l%16][8(l/16) .. +8], B[8(l/16) .. +8][l%16];
+// accumulator element i of lane l is D[4(l/16) + i][l%16].
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Direct global-to-LDS load of 16 B per lane (see lds_dma16) from a scalar base and a lane offset in bytes. The base has to be settled (no VALU
+// instruction may write it in the five wait states before): callers compute it with scalar arithmetic.
+__device__ __forceinline__ void lds_dma16_row(const void* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(lds_base)
+               : "memory", "m0");
+}
+
 // The running maximum starts at the lowest finite value, not at -inf: a row that has seen nothing yet
 // (and one that never will) then keeps all its exponentials at exp2(-inf) = 0, with no inf - inf.
 constexpr float kLowest = -3.402823466e38f;
@@ -218,11 +233,26 @@ struct PagedWriteArgs : WriteArgs {
 struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
+  uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), or nullptr (wide kernel)
   float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
   int32_t cost;        // counts of a block beyond its units
 };
+
+// The second bf16 term of four values of q_cat (their first has been, or is, rounded from them), where the
+// call keeps one; both terms of a pair.
+__device__ __forceinline__ void paged_q_lo(const PagedAttendArgs& a, int64_t at, f32x4 v) {
+  if (a.q_lo)
+    *reinterpret_cast<bf16x4*>(a.q_lo + at) = to_bf16x4(v - __builtin_convertvector(to_bf16x4(v), f32x4));
+}
+__device__ __forceinline__ void paged_q_pair(const PagedAttendArgs& a, int64_t at, float u, float v) {
+  const uint16_t hu = to_bf16_bits(u), hv = to_bf16_bits(v);
+  *reinterpret_cast<uint32_t*>(a.qcat + at) = (uint32_t)hu | (uint32_t)hv << 16;
+  if (a.q_lo)
+    *reinterpret_cast<uint32_t*>(a.q_lo + at) = (uint32_t)to_bf16_bits(u - bf16_bits_to_f32(hu)) |
+                                                (uint32_t)to_bf16_bits(v - bf16_bits_to_f32(hv)) << 16;
+}
 
 constexpr int kPagedMaxSeqs = 4096;
 
@@ -237,6 +267,7 @@ void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, in
 // The kernel of many rows per block (k_paged_wide.hip): its block, 0 where it is not built, and launch.
 int paged_wide_rows(int d_c, int d_rope);
 hipError_t launch_paged_attend_wide(const PagedAttendArgs& a, hipStream_t s);
+hipError_t launch_paged_attend_wide512(const PagedAttendArgs& a, hipStream_t s);
 
 constexpr int kCopyPairs = 440;  // page pairs per launch: they travel in the kernel's arguments
 struct PagesCopyArgs {
