@@ -410,7 +410,7 @@ int videomla_dense_attend(const videomla_dims* dims, const videomla_window* win,
  * and are left as they are.
  *
  *   n_seqs         sequences, 1 .. 4096
- *   n_tokens       rows of x, q_nope, q_r and out
+ *   n_tokens       rows of x, q_nope, q_r and out, at least 1
  *   page_tokens    tokens per page (any number)
  *   max_pages      columns of the block table; max_pages * page_tokens <= 2^30
  *   n_pages        pages of the pool; n_pages * page_tokens < 2^31
@@ -461,7 +461,8 @@ int videomla_paged_cache_write(const videomla_dims* dims, const videomla_paged* 
                                void* stream);
 
 /* Bytes of device workspace videomla_paged_attend needs (0 if the arguments are invalid or not
- * supported). The device arrays are not read: their pointers may be NULL here. */
+ * supported). The device arrays are not read: their pointers may be NULL here. A workspace of this size
+ * also serves calls that differ in a smaller max_new only. */
 size_t videomla_paged_attend_workspace_bytes(const videomla_dims* dims, const videomla_paged* paged);
 
 /*

@@ -1018,8 +1018,6 @@ int videomla_attend_layer(const videomla_dims* d, const videomla_window* w, int3
   return ok();
 }
 
-// ---- timers -------------------------------------------------------------------------------------
-
 // ---- paged cache ----------------------------------------------------------------------------------
 }  // extern "C"
 
@@ -1079,11 +1077,14 @@ int check_paged_attend_shape(const videomla_dims* d, const videomla_paged* p) {
   return VIDEOMLA_OK;
 }
 
-PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
+int64_t paged_max_rows(const videomla_dims* d, const videomla_paged* p) {
+  return (p->max_new > 0 && p->max_new < p->n_tokens ? p->max_new : p->n_tokens) * (int64_t)d->n_heads;
+}
+
+PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p, int64_t max_rows) {
   PagedLayout L{};
   const int64_t rows = (int64_t)p->n_tokens * d->n_heads;
-  const int64_t max_new = p->max_new > 0 && p->max_new < p->n_tokens ? p->max_new : p->n_tokens;
-  paged_attend_shape(d->d_c, d->d_rope, max_new * d->n_heads, &L.rows, &L.unit, &L.cost);
+  paged_attend_shape(d->d_c, d->d_rope, max_rows, &L.rows, &L.unit, &L.cost);
   // a sequence's last block may be partly filled; sequences without rows have none
   L.max_blocks = (int32_t)(rows / L.rows + (p->n_seqs < p->n_tokens ? p->n_seqs : p->n_tokens));
   L.n_wg = device_cu_count();
@@ -1106,6 +1107,16 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p) {
   L.work_block = take((size_t)L.n_wg * sizeof(PagedBlock));
   L.total = at;
   return L;
+}
+
+// What the call needs with its max_new or any smaller one, so that a workspace made for a batch's largest
+// chunk serves the single-token steps after it: the row blocks are 16, up to 32, or the wide kernel's rows.
+size_t paged_workspace_bytes(const videomla_dims* d, const videomla_paged* p) {
+  const int64_t most = paged_max_rows(d, p);
+  size_t need = 0;
+  for (int64_t r : {(int64_t)16, (int64_t)32, most})
+    if (r <= most || r == 16) need = std::max(need, paged_layout(d, p, r).total);
+  return need;
 }
 
 }  // namespace
@@ -1139,7 +1150,7 @@ int videomla_paged_cache_write(const videomla_dims* d, const videomla_paged* p, 
 
 size_t videomla_paged_attend_workspace_bytes(const videomla_dims* d, const videomla_paged* p) {
   if (check_paged_attend_shape(d, p)) return 0;
-  return paged_layout(d, p).total;
+  return paged_workspace_bytes(d, p);
 }
 
 int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const uint16_t* q_nope,
@@ -1153,8 +1164,8 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   if (!aligned16(q_nope) || !aligned16(q_r) || !aligned16(w_uk) || !aligned16(w_uv) ||
       !aligned16(c_kv) || !aligned16(k_r) || !aligned16(out))
     return fail(VIDEOMLA_EALIGN, "tensor pointers must be 16-byte aligned");
-  const PagedLayout L = paged_layout(d, p);
-  if (int e = check_workspace(workspace, workspace_bytes, L.total)) return e;
+  const PagedLayout L = paged_layout(d, p, paged_max_rows(d, p));
+  if (int e = check_workspace(workspace, workspace_bytes, paged_workspace_bytes(d, p))) return e;
   char* ws = static_cast<char*>(workspace);
   PagedAttendArgs a{};
   a.q_nope = q_nope; a.q_r = q_r; a.w_uk = w_uk; a.w_uv = w_uv; a.c_kv = c_kv; a.k_r = k_r; a.out = out;
