@@ -72,29 +72,40 @@ __device__ __forceinline__ void sum_wave_parts(const float* part, int stride, in
 // The paged write's tokens t0 + lane (lanes below n): absolute positions, and the table entry that names
 // each one's page, loaded without waiting for it. The sequences of the workgroup's rows are walked in
 // order with uniform (scalar) loads, each lane keeping the values of its own: a search per lane would
-// wait for every weight and activation load in flight. `page` is then read when the row is stored.
+// wait for every weight and activation load in flight. `page` is then read when the row is stored. Only
+// sequences with rows here are visited: past one without rows the next is looked for by halving.
 struct PagedToken {
   int32_t index;   // index in the sequence's cached tokens; < 0: not to be written
   int32_t page;    // page id as the table has it
   TokenPos pos;
 };
 __device__ __forceinline__ PagedToken paged_token(const PagedGeo& g, int t0, int n, int lane_tok, bool live) {
-  int lo = 0, hi = g.n_seqs;  // the first sequence that ends behind t0
-  while (lo < hi) {
-    const int m = (lo + hi) >> 1;
-    if (paged_read<true>(g.cu, m + 1) > t0) hi = m;
-    else lo = m + 1;
-  }
+  int at_row = t0;
+  auto next = [&](int s) {  // the first sequence from s on that ends behind at_row
+    int hi = g.n_seqs;
+    while (s < hi) {
+      const int m = (s + hi) >> 1;
+      if (paged_read<true>(g.cu, m + 1) > at_row) hi = m;
+      else s = m + 1;
+    }
+    return s;
+  };
   int32_t seq = 0, index = -1;
   int64_t first = 0;
-  for (int s = lo; s < g.n_seqs; ++s) {
+  for (int s = next(0); s < g.n_seqs;) {
     const PagedSeq q = paged_seq<true>(g, s);
-    if (q.lo >= t0 + n) break;
+    if (q.hi <= at_row) {
+      s = next(s + 1);
+      continue;
+    }
     if (lane_tok >= q.lo && lane_tok < q.hi) {
       seq = s;
       index = q.kv - (q.hi - lane_tok);
       first = q.first;
     }
+    at_row = q.hi;
+    ++s;
+    if (at_row >= t0 + n) break;
   }
   PagedToken r;
   r.index = live ? index : -1;
