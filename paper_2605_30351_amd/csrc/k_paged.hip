@@ -20,7 +20,7 @@ typedef __attribute__((address_space(3))) int32_t lds_i32;
 
 // Direct global-to-LDS load of 4 B per lane: lane l's word lands at lds_base + 4 l (see lds_dma16).
 __device__ __forceinline__ void lds_dma4(const int32_t* gptr, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
                :
                : "v"(gptr), "s"(lds_base)
                : "memory", "m0");
@@ -136,9 +136,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int r = row0 + 16 * qb + l16;
-      see_b[qb] = 0;
-      see_e[qb] = 0x7fffffff;
-      if (r < n_rows) paged_row_sees(g, pb, H, 16 * qb + l16, see_b[qb], see_e[qb]);
+      paged_row_sees(g, pb, H, min(16 * qb + l16, n_rows - 1 - row0), see_b[qb], see_e[qb]);  // (past the end: as the last)
       auto own_row = [&](const uint16_t* q, bf16x8 (&v)[C::KS]) {
         const uint16_t* src = q + ((int64_t)pb.lo * H + (r < n_rows ? r : row0)) * C::DQKP + 8 * gq;
 #pragma unroll

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
 
     // queries, B-operand layout: lane holds row l32, dims 16 ks + 8 g .. +8; and what that row sees
     bf16x8 q[C::KS];
-    int see_b = 0, see_e = 0x7fffffff;
+    int see_b, see_e;
     const int r_own = row0 + l32;
     {
       const bool live = r_own < n_rows;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
         if (!live) v = u32x4{0, 0, 0, 0};
         q[ks] = as_bf16x8(v);
       }
-      if (live) paged_row_sees(pg, pb, H, wave * 32 + l32, see_b, see_e);
+      paged_row_sees(pg, pb, H, min(wave * 32 + l32, n_rows - 1 - pb.row0), see_b, see_e);  // (past the end: as the last)
     }
     // rows are in token order: the limits of the wave's first and last row hold for all
     const int b_max = __builtin_amdgcn_readlane(see_b, max(min(n_rows - 1 - row0, 31), 0));

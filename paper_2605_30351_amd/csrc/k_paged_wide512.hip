@@ -120,9 +120,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_attend_wide512_kernel(co
         if (r >= n_rows) v = u32x4{0, 0, 0, 0};
         q[rb][ks] = as_bf16x8(v);
       }
-      see_b[rb] = 0;
-      see_e[rb] = 0x7fffffff;
-      if (r < n_rows) paged_row_sees(pg, pb, H, rr, see_b[rb], see_e[rb]);
+      paged_row_sees(pg, pb, H, min(rr, n_rows - 1 - row0), see_b[rb], see_e[rb]);  // (past the end: as the last)
     }
     f32x4 o[4][8];  // rows 16 rb .., columns 128 wave + 16 d ..
     float m_run[2] = {kLowest, kLowest}, l_run[2] = {0.f, 0.f};

@@ -60,9 +60,11 @@ typedef __attribute__((address_space(3))) void lds_void;
 // Direct global-to-LDS load of 16 B per lane: lane l's bytes land at LDS address lds_base + 16 l.
 // Issued as inline assembly so that the compiler does not treat it as an LDS write it must wait
 // for before every LDS read and barrier; the callers order it with explicit vmcnt waits (the
-// load counts as one outstanding vector-memory operation until its data is in LDS).
+// load counts as one outstanding vector-memory operation until its data is in LDS). An instruction that
+// uses m0 for LDS needs one wait state behind the scalar write of m0, which the compiler does not put into
+// inline assembly either: without it a load can go to the place of the one before.
 __device__ __forceinline__ void lds_dma16(const uint16_t* gptr, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
                : "v"(gptr), "s"(lds_base)
                : "memory", "m0");

@@ -130,10 +130,11 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Direct global-to-LDS load of 16 B per lane (see lds_dma16) from a scalar base and a lane offset in bytes. The base has to be settled (no VALU
-// instruction may write it in the five wait states before): callers compute it with scalar arithmetic.
+// Direct global-to-LDS load of 16 B per lane (see lds_dma16) from a scalar base and a lane offset in bytes.
+// The base has to be settled (no VALU instruction may write it in the five wait states before): callers
+// compute it with scalar arithmetic.
 __device__ __forceinline__ void lds_dma16_row(const void* base, uint32_t off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
                : "v"(off), "s"(base), "s"(lds_base)
                : "memory", "m0");
@@ -191,12 +192,14 @@ struct PagedBlock {
 static_assert(sizeof(PagedBlock) == 64, "one scalar load");
 
 // The keys [b, e) that row r of the block (counted from its first row) sees. A block's rows are at most
-// 256 tokens, so that only mask blocks below that length are crossed more than once.
+// 256 tokens, so that only mask blocks below that length are crossed more than once. Without a branch that
+// lanes take differently: where such a branch rejoined in a kernel that fills the register file, the
+// compiler moved another value for the lanes in it only.
 __device__ __forceinline__ void paged_row_sees(const PagedGeo& g, const PagedBlock& p, int H, int r,
                                                int32_t& b, int32_t& e) {
   const int d = (p.head0 + r) / H - p.to_next;  // tokens past the first boundary
-  int64_t off = 0;
-  if (d >= 0) off = (1 + (g.mask_block <= 256 ? d / (int)g.mask_block : 0)) * g.mask_block;
+  const int more = g.mask_block <= 256 ? max(d, 0) / max((int)g.mask_block, 1) : 0;
+  const int64_t off = (d >= 0 ? 1 + more : 0) * g.mask_block;
   const int64_t end = p.end0 + off, beg = p.beg0 + off;
   e = (int32_t)(end < 0 ? 0 : end > p.kv ? p.kv : end);
   b = (int32_t)(beg < 0 ? 0 : beg > e ? e : beg);
@@ -209,7 +212,7 @@ struct PagedWork {
 // Where a row's latents are, written by the workgroup that has its block's first unit (the absorb kernel
 // clears it): ns workgroups share its block, w0 the first of them, row its place in the block; ns 1: its
 // row of o_lat; ns 0: the row belongs to no sequence.
-struct PagedRow {
+struct alignas(8) PagedRow {  // (one store: rows that bad offsets give to two blocks have either's record)
   int32_t w0;
   uint16_t ns, row;
 };

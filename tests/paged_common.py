@@ -146,6 +146,49 @@ class Batch:
         return np.array(rows, int), c, rope(d, x @ f(self.w_kr).T, np.array(pos, int))
 
 
+def attention_by_sequence(b, device):
+    """Batch.attention for calls of many tokens: the same sums in torch, all heads' keys and values of a
+    sequence at once, its tokens in blocks."""
+    d, H = b.dims, b.dims.n_heads
+    f = lambda a: torch.from_numpy(bf16_to_f64(a)).to(device)  # noqa: E731
+    uk, uv = f(b.w_uk).view(H, d.d_nope, d.d_c), f(b.w_uv).view(H, d.d_v, d.d_c)
+    ckv, kr = f(b.c_kv).view(-1, d.d_c), f(b.k_r).view(-1, d.d_rope)
+    scale = d.softmax_scale or (d.d_nope + d.d_rope) ** -0.5
+    out = np.full((b.rows, H, d.d_v), np.nan)
+    bound = np.zeros_like(out)
+    for s in range(len(b.seqs)):
+        lo, hi, kv = int(b.cu[s]), int(b.cu[s + 1]), int(b.kv[s])
+        rows = np.array([b.pool_row(s, j) for j in range(kv)], int)
+        first = int(b.first[s]) if b.with_first else 0
+        if kv == 0:
+            out[lo:hi] = 0
+            continue
+        c, k = ckv[rows], kr[rows]
+        for t0 in range(lo, hi, 32):
+            toks = np.arange(t0, min(t0 + 32, hi))
+            at = kv - hi + toks
+            see = torch.zeros(len(toks), kv, dtype=torch.bool)
+            for n, i in enumerate(at):
+                see[n, b.seen(s, int(i))] = True
+            see = see.to(device)
+            qr = torch.from_numpy(rope(d, bf16_to_f64(b.q_r[toks]), np.maximum(0, first + at)[:, None])).to(device)
+            qn = f(b.q_nope[toks])
+            for h in range(H):
+                lat = qn[:, h] @ uk[h]
+                sc = ((lat @ c.t() + qr[:, h] @ k.t()) * scale).masked_fill(~see, -np.inf)
+                ds = (lat.abs() @ c.abs().t() + qr[:, h].abs() @ k.abs().t()) * (U * scale)
+                ds = ds.masked_fill(~see, 0.0)
+                p = torch.where(see.any(1, keepdim=True), sc.softmax(1), 0.0)
+                v = c @ uv[h].t()
+                o = p @ v
+                rel = ds + ds.amax(1, keepdim=True) + 2 * U
+                moved = ((p * rel)[..., None] * (v[None] - o[:, None]).abs()).sum(1)
+                rounds = U * ((p @ c).abs() @ uv[h].abs().t() + o.abs())
+                out[toks, h] = o.cpu().numpy()
+                bound[toks, h] = torch.where(see.any(1, keepdim=True), 2 * (moved + rounds) + 1e-6, 0.0).cpu().numpy()
+    return out, bound
+
+
 def assert_within(got, want, bound, label):
     """got (bf16 values) within the bound of every value, and 1e-2 of the whole in the 2-norm."""
     live = ~np.isnan(want)

@@ -5,6 +5,7 @@ import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 
 from tests._build_once import ensure_built
@@ -180,3 +181,21 @@ int main() {
     assert r.returncode == 0, r.stderr[-2000:]
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stdout
+
+
+@pytest.mark.parametrize("mask,window", [(0, 0), (1, 5), (7, 0)])
+def test_the_two_forms_of_the_definition_agree(mask, window):
+    from tests.paged_common import Batch, attention_by_sequence
+    b = Batch(TINY, [(3, 3, 0), (0, 4, 1), (2, 1, 0), (40, 50, 1000), (1, 0, 0)], page=4, pad=2, mask=mask, window=window,
+              seed=3, holes=[(3, 2, -1)])
+    for one, two in zip(b.attention(), attention_by_sequence(b, "cpu")):
+        assert np.allclose(one, two, rtol=1e-9, atol=1e-12, equal_nan=True)
+
+
+@pytest.mark.parametrize("d", [TINY, *WAN_DC.values()], ids=lambda d: f"dc{d.d_c}")
+@pytest.mark.parametrize("tokens", [1, 3, 40, 5000, 3000000])
+def test_a_workspace_serves_every_smaller_bound_on_the_new_tokens(d, tokens):
+    size = lambda m: L.raw().videomla_paged_attend_workspace_bytes(  # noqa: E731
+        ctypes.byref(dims(d)), ctypes.byref(paged(n_tokens=tokens, n_seqs=1, max_new=m)))
+    sizes = [size(m) for m in (1, 2, 3, 8, 40, 5000, 0)]
+    assert 0 < sizes[0] and sizes == sorted(sizes)
