@@ -164,6 +164,18 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
     }
     if (c0 == 0) VMLA_STAMP(a, kStampQAbsorb, 2);
     if (STAGE) __syncthreads();  // every wave is done reading W_UK_h: its area holds the rows
+    [[maybe_unused]] bool with_lo = ok;  // this token's second terms are wanted
+    if constexpr (PAGED && STAGE) {
+      if (a.unit == 32) {
+        float n2 = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (cb * 32 + 8 * (i >> 2) < DC) n2 += acc[cb][i] * acc[cb][i];
+        with_lo = ok && half_swap_sum(n2) * a.qscale * a.qscale > 0.9f * kOneTerm * kOneTerm;
+      }
+    }
     if (ok || STAGE) {
 #pragma unroll
       for (int cb = 0; cb < NCB; ++cb)
@@ -175,7 +187,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
                              acc[cb][4 * i + 2] * a.qscale, acc[cb][4 * i + 3] * a.qscale};
             *reinterpret_cast<bf16x4*>(STAGE ? ot + l32 * OS + c : dst + c) = to_bf16x4(v);
             if constexpr (PAGED) {
-              if (ok) paged_q_lo(a, (int64_t)row * DQKP + c, v);
+              if (with_lo) paged_q_lo(a, (int64_t)row * DQKP + c, v);
             }
           }
         }

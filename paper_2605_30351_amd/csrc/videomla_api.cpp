@@ -1096,7 +1096,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p, int64_
     return off;
   };
   L.qcat = take((size_t)rows * qk * 2);
-  L.q_lo = L.unit > 32 ? take((size_t)rows * qk * 2) : 0;  // (the few-row kernel)
+  L.q_lo = L.unit == 32 && d->d_c == 512 ? 0 : take((size_t)rows * qk * 2);
   L.o_lat = take((size_t)rows * d->d_c * 4);
   L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
   L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);

@@ -236,12 +236,17 @@ struct PagedWriteArgs : WriteArgs {
 struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
-  uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), or nullptr (wide kernel)
+  uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), or nullptr (512-wide kernel)
   float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
   int32_t cost;        // counts of a block beyond its units
 };
+
+// The wide kernel takes the second term of rows whose latent part of q_cat is longer than this, in exponents
+// of 2 (against latents of unit RMS: a standard deviation of the scores); the absorption writes it for these
+// and, as it compares before the rounding, for those just below.
+constexpr float kOneTerm = 2.3f;
 
 // The second bf16 term of four values of q_cat (their first has been, or is, rounded from them), where the
 // call keeps one; both terms of a pair.

@@ -86,3 +86,24 @@ def test_two_graphs_share_a_workspace():
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(host_bits(out), want[n % 2]), n
+
+
+@pytest.mark.parametrize("max_new", [0, 1])
+@pytest.mark.parametrize("dims", WIDTHS[1:5], ids=IDS[1:5])
+def test_long_queries_keep_their_precision(dims, max_new):
+    """Scores of standard deviation 4 in every other token, 1 in the rest. With both terms of a long query the
+    roundings left are the weights' and the output's own: a weight is off by as much of itself as the output
+    is, so that the two together are at most sqrt(2) times the output's rounding in the 2-norm (one term alone
+    measures 2.2 times); 1.5 for the sums. The short queries' rounding adds as much as their output's."""
+    seqs = [(301, 900, 0), (61, 200, 7), (3, 40, 0)]
+    b, short = (Batch(dims, seqs, page=48, mask=1, seed=36, gain=g, max_new=max_new) for g in (4.0, 1.0))
+    for long_q, short_q in ((b.q_nope, short.q_nope), (b.q_r, short.q_r)):
+        long_q[1::2] = short_q[1::2]
+    want, bound = attention_by_sequence(b, "cuda")
+    got = bf16_to_f64(host_bits(attend(b)))
+    assert_within(got, want, bound, f"{dims.d_c}")
+    rounded = torch.from_numpy(want).to(torch.bfloat16).double().numpy()
+    for name, part, most in (("long", slice(0, None, 2), 1.5), ("short", slice(1, None, 2), 1.5 * 2 ** 0.5)):
+        off = [np.linalg.norm(v[part] - want[part]) for v in (got, rounded)]
+        print(f"{dims.d_c} {name}: {off[0] / off[1]:.3f} of the output's rounding", flush=True)
+        assert off[0] <= most * off[1], (name, off)
