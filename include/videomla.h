@@ -475,8 +475,9 @@ size_t videomla_paged_attend_workspace_bytes(const videomla_dims* dims, const vi
  *   out        [n_tokens][n_heads][d_v]      bf16
  *   workspace  device buffer of at least videomla_paged_attend_workspace_bytes() bytes; every call
  *              writes what it reads there, so that calls ordered on one stream may share one
- * Arithmetic, shapes and errors of videomla_attend. Results are bitwise reproducible. Infinities and
- * NaN in tokens that a query does not see do not reach it.
+ * Arithmetic, shapes and errors of videomla_attend, but for the absorbed queries: they are multiplied as
+ * two bf16 terms in calls of few rows per sequence and, up to d_c = 256, wherever one is long. Results are
+ * bitwise reproducible. Infinities and NaN in tokens that a query does not see do not reach it.
  */
 int videomla_paged_attend(const videomla_dims* dims, const videomla_paged* paged,
                           const uint16_t* q_nope, const uint16_t* q_r, const uint16_t* w_uk,
