@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
 
       // Both terms of the absorbed queries: one alone is off by up to 2^-8 of each component, which moves a
       // score of size |s| by about 2^-9.5 |s| and weighs most where the softmax is peaked (scores of standard
-      // deviation 4: outputs off by 0.0044 in the 2-norm with one term, 0.0025 with two). These matrix steps
+      // deviation 4: outputs off by 0.0044 in the 2-norm with one term, 0.0018 with two). These matrix steps
       // pass under the loads of the keys, which bound this kernel.
       f32x4 s[QB][2];
 #pragma unroll
@@ -631,8 +631,9 @@ __global__ __launch_bounds__(256, DC <= 192 ? 4 : DC <= 256 ? 3 : 2) void paged_
 
 namespace {
 // 16-row blocks per workgroup of the few-row kernel, at most: beyond, the wide kernel is as fast or faster. us,
-// few / wide, d_c = 192: 24 rows x 8 sequences of up to 16,000 keys 17.2 / 14.4, up to 32,760 31.2 / 35.0; 48 rows
-// 23.9 / 15.6 and 45.1 / 37.9. At d_c = 256 and 512 two blocks' accumulators and queries do not fit.
+// few / wide, d_c = 192: 24 rows x 8 sequences of 16,000 keys 22.1 / 20.6, of 32,760 32.6 / 32.3, x 32 of 2,000 to
+// 32,760 52.4 / 62.1; 48 rows x 8 of 3,000 to 16,000 22.6 / 19.0, to 32,760 31.9 / 23.7. At d_c = 256 and 512 two
+// blocks' accumulators and queries do not fit.
 constexpr int few_most(int dc) { return dc <= 192 ? 2 : 1; }
 }  // namespace
 

@@ -12,6 +12,10 @@
 // barrier, agree on the new maxima, take the probabilities again and rescale.
 // Per tile and workgroup: 66 MFMAs a wave (1,056 cycles) over 68 KB of K and 32 KB of V reads (780 cycles at
 // 128 bytes a cycle).
+//
+// Queries are one bf16 term, however long: outputs are off by 0.0042 in the 2-norm at scores of standard
+// deviation 4 (0.0026 at 1). Neither registers nor LDS hold the second terms of 64 rows; read from the cache
+// for every tile they take 1,560 tokens over 8,000 keys from 414 to 2,077 us.
 #include <type_traits>
 
 #include "vmla_paged.h"
