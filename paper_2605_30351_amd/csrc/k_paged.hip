@@ -265,9 +265,20 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
         }
       }
       if (masked) {
+        float least = s[0][0][0];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) least = fminf(least, s[qb][i >> 2][i & 3]);
+        uint32_t bad = 0;
+        if (__builtin_amdgcn_ballot_w64(least == kMasked) != 0)
+          bad = not_finite_keys<DC / 8>([&](int r, int c) {
+            return tile + r * C::STRIDE + (c ^ (C::SPLIT ? C::swz16(r) : C::swz(r))) * 8;
+          });
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-          const uint32_t seen = seen_keys(there, see_b[qb] - k0, see_e[qb] - k0) >> (4 * gq);
+          const uint32_t sees = seen_keys(there, see_b[qb] - k0, see_e[qb] - k0), seen = sees >> (4 * gq);
+          l_run[qb] = sees & bad ? kNotANumber : l_run[qb];
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             s[qb][i >> 2][i & 3] = seen >> (16 * (i >> 2) + (i & 3)) & 1 ? s[qb][i >> 2][i & 3] : kMasked;

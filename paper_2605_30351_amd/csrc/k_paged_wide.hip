@@ -45,18 +45,12 @@ struct WideCfg {
   static_assert(DQKP % 32 == 0 && 32 * CPR % 64 == 0 && DVB * 32 <= DQKP, "tile shape");
 };
 
-// The lane, computed where it is used: kept over the main loop it would cost a register that is not there.
-__device__ __forceinline__ int lane_here() {
-  uint32_t zero = 0;
-  asm volatile("" : "+s"(zero));
-  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
-}
-
 template <int DC, int DR, int NW>
 __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const PagedAttendArgs a) {
   using C = WideCfg<DC, DR, NW>;
   __shared__ __attribute__((aligned(16))) uint16_t tile[3][C::TILE];
   __shared__ __attribute__((aligned(16))) uint16_t q_lo[NW][C::KS][64 * 8];  // each wave's second term, by lane
+  __shared__ uint32_t cleared;  // keys of the tile in work, between settle()'s barriers
   __shared__ __attribute__((aligned(16))) float resc[C::RESC_LDS ? NW : 1][C::RESC_LDS ? 64 * 16 : 4];
 
   const int lane = threadIdx.x & 63;
@@ -66,6 +60,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const int H = a.n_heads;
   const PagedWork wk = paged_read<true>(a.plan.work, blockIdx.x);
   int left = wk.n, blk = wk.block, end = wk.end;
+  if (threadIdx.x == 0) cleared = 0;
 
   // this wave's loads j = wave + NW i of a tile: where this lane's chunk is in pool row 0 of c_kv, or of k_r
   // (the pad reads k_r again, against zeros in q_cat); the tile row, and the bytes of a pool row
@@ -156,22 +151,26 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     // rows are in token order: the limits of the wave's first and last row hold for all
     const int b_max = __builtin_amdgcn_readlane(see_b, max(min(n_rows - 1 - row0, 31), 0));
     const int e_min = __builtin_amdgcn_readfirstlane(see_e);
+    f32x16 o[C::DVB];
+    float m_run = kLowest, l_run = 0.f, spoiled = 0.f, own_max;
+#pragma unroll
+    for (int d = 0; d < C::DVB; ++d) o[d] = f32x16{};
+
     // the latents of tile t in buf, made finite if some row of the block does not see one of its keys
     // (called by all waves, after every wave has used the tile's K and before any uses its V)
+    // A row that sees a latent that was not finite is spoiled: its sum becomes NaN.
     auto settle = [&](int t, uint32_t keys, uint16_t* buf) {
       const int k0 = key0 + t * 32;
       if (keys == 0xffffffffu && k0 >= pb.all_b && k0 + 32 <= pb.all_e) return;
-      for (int i = wave * 64 + lane_here(); i < 32 * C::CPR; i += NW * 64) {
-        u32x4* p = reinterpret_cast<u32x4*>(buf + i * 8);
-        *p = as_u32x4(finite_or_zero(as_bf16x8(*p)));
+      for (int i0 = wave * 64; i0 < 32 * C::CPR; i0 += NW * 64) {
+        const int i = i0 + lane_here();
+        clear_not_finite(buf + i * 8, &cleared, [&] {
+          const int r = i / C::CPR;
+          return C::pos(r, i % C::CPR) < DC / 8 ? 1u << r : 0u;
+        });
       }
-      __syncthreads();
+      if (seen_keys(keys, see_b - k0, see_e - k0) & cleared_keys(&cleared)) spoiled = kNotANumber;
     };
-
-    f32x16 o[C::DVB];
-    float m_run = kLowest, l_run = 0.f, own_max;
-#pragma unroll
-    for (int d = 0; d < C::DVB; ++d) o[d] = f32x16{};
 
     auto masked_tile = [&](uint32_t keys, int k0) { return keys != 0xffffffffu || k0 < b_max || k0 + 32 > e_min; };
     auto mask = [&](f32x16& s, uint32_t keys, int k0) {
@@ -349,7 +348,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       else steps(std::false_type{});
 
       // ---- a whole block's latents, or this segment's partial result ----
-      const float l = half_swap_sum(l_run);
+      const float l = half_swap_sum(l_run + spoiled);
       if (r_own < n_rows) {
         const bool whole = n_tiles == pb.n_units;
         const int64_t prow = (2 * (int64_t)blockIdx.x + (u0 == 0)) * C::ROWS + wave * 32 + l32;

@@ -39,6 +39,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_attend_wide512_kernel(co
   __shared__ float tile_max[2][kRows];  // per key half
   __shared__ float factor[kRows], sums[2][kRows];
   __shared__ int grown[3];
+  __shared__ uint32_t cleared;  // keys of the tile in work, between settle()'s barriers
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -48,6 +49,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_attend_wide512_kernel(co
   const int H = a.n_heads;
   const PagedWork wk = paged_read<true>(a.plan.work, blockIdx.x);
   int left = wk.n, blk = wk.block, end = wk.end;
+  if (threadIdx.x == 0) cleared = 0;
 
   // K operand of k-step ks: row 16 kh + l16, chunk 4 ks + gq; V^T: rows 4 gq + l16 / 4 (+ 16), columns
   // 128 wave + 16 d + 4 (l16 % 4); a few bases reach every step with immediate offsets
@@ -134,14 +136,16 @@ __global__ __launch_bounds__(64 * kWaves, 1) void paged_attend_wide512_kernel(co
       for (int d = 0; d < 8; ++d) o[rb][d] = f32x4{};
 
     // the latents of tile t in buf, made finite if a key is missing or some row of the block does not see one
+    // A row that sees a latent that was not finite gets a NaN sum.
     auto settle = [&](int t, uint32_t keys, uint16_t* buf) {
       const int k0 = key0 + t * 32;
       if (keys == 0xffffffffu && k0 >= pb.all_b && k0 + 32 <= pb.all_e) return;
-      for (int i = threadIdx.x; i < 32 * kDC / 8; i += 64 * kWaves) {
-        u32x4* p = reinterpret_cast<u32x4*>(buf + i * 8);
-        *p = as_u32x4(finite_or_zero(as_bf16x8(*p)));
-      }
-      __syncthreads();
+      for (int i = threadIdx.x; i < 32 * kDC / 8; i += 64 * kWaves)
+        clear_not_finite(buf + i * 8, &cleared, [&] { return 1u << (i / (kDC / 8)); });
+      const uint32_t bad = cleared_keys(&cleared);
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+        l_run[rb] = seen_keys(keys, see_b[rb] - k0, see_e[rb] - k0) & bad ? kNotANumber : l_run[rb];
     };
     // S^T of this wave's rows and keys: two chains of matrix steps per row block, so that few wait for the
     // last, K read three steps ahead, and between(ks) after each step: the loads of a later tile go out there

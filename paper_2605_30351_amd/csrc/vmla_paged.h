@@ -152,9 +152,16 @@ __device__ __forceinline__ uint32_t seen_keys(uint32_t keys, int b, int e) {
   return keys & (uint32_t)(((uint64_t)1 << hi) - ((uint64_t)1 << min(lo, hi)));
 }
 
+// The lane, computed where it is used: kept over the main loop it would cost a register that is not there.
+__device__ __forceinline__ int lane_here() {
+  uint32_t zero = 0;
+  asm volatile("" : "+s"(zero));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+}
+
 // bf16 values with infinities and NaN replaced by zero. In a tile that is masked for some row, a key's
 // probability may be 0 while its latent is not finite, and 0 * NaN would reach the rows that do not see
-// it; a row that does see it has a NaN score, since the latent is part of the key.
+// it. The rows that do see it get a NaN sum instead: 0 * inf or inf - inf, whatever the sign of the score.
 __device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 v) {
   u32x4 u = as_u32x4(v);
 #pragma unroll
@@ -164,6 +171,50 @@ __device__ __forceinline__ bf16x8 finite_or_zero(bf16x8 v) {
     u[i] = lo | hi;
   }
   return as_bf16x8(u);
+}
+// Whether some of them are (an exponent of all ones carries into the sign's place).
+__device__ __forceinline__ bool not_finite(u32x4 u) {
+  const uint32_t e = 0x7f807f80u, one = 0x00800080u;
+  return (((u[0] & e) + one | (u[1] & e) + one | (u[2] & e) + one | (u[3] & e) + one) & 0x80008000u) != 0;
+}
+constexpr float kNotANumber = __builtin_nanf("");
+
+// Of a tile's 32 keys those whose latents are not all finite; chunk_at(key, c): where 8 of them are. For waves
+// that clear the latents in registers, called where some score is minus infinity, as it is with such a latent
+// if it is not NaN or plus infinity (which make the sum NaN by themselves). An infinite k^R makes such scores
+// too, with finite latents: a key of no weight.
+template <int CHUNKS, class At>
+__device__ __forceinline__ uint32_t not_finite_keys(At chunk_at) {
+  const int lane = lane_here();
+  uint64_t bad = 0;
+#pragma unroll 1
+  for (int c = 0; c < CHUNKS; c += 2)
+    bad |= __builtin_amdgcn_ballot_w64(not_finite(*reinterpret_cast<const u32x4*>(chunk_at(lane & 31, c + (lane >> 5)))));
+  return (uint32_t)bad | (uint32_t)(bad >> 32);
+}
+
+// For workgroups that clear them in LDS: 8 values, a lane, made finite in place. The bits key() of those that
+// were not are added to `word`.
+template <class Key>
+__device__ __forceinline__ void clear_not_finite(uint16_t* p, uint32_t* word, Key key) {
+  u32x4* const at = reinterpret_cast<u32x4*>(p);
+  const u32x4 v = *at;
+  const bool bad = not_finite(v);
+  if (__builtin_amdgcn_ballot_w64(bad) == 0) return;
+  *at = as_u32x4(finite_or_zero(as_bf16x8(v)));
+  // (of an atomic OR the compiler makes a loop over the lanes)
+  asm volatile("ds_or_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : : "v"(lds_addr(word)), "v"(bad ? key() : 0u) : "memory");
+}
+// Behind it, by all waves: the cleared latents visible, and the keys. `word` was 0 and is left so; the callers
+// have a barrier between two rounds.
+__device__ __forceinline__ uint32_t cleared_keys(uint32_t* word) {
+  __syncthreads();
+  const uint32_t keys = __builtin_amdgcn_readfirstlane(*word);
+  if (keys != 0) {
+    __syncthreads();  // every wave has read it
+    if (threadIdx.x == 0) *word = 0;
+  }
+  return keys;
 }
 
 // The plan of one attention call, in the workspace: written beside the absorbed queries (paged_plan),
