@@ -478,7 +478,8 @@ size_t videomla_paged_attend_workspace_bytes(const videomla_dims* dims, const vi
  * Arithmetic, shapes and errors of videomla_attend, but for the absorbed queries: they are multiplied as
  * two bf16 terms in calls of few rows per sequence and, up to d_c = 256, wherever one is long. Results are
  * bitwise reproducible. Infinities and NaN in tokens that a query does not see do not reach it; in the
- * latents of a token that it sees they make its result NaN, as 0 * inf and inf - inf do.
+ * latents of a token that it sees they make its result NaN, as 0 * inf and inf - inf do. A token whose
+ * score is minus infinity (of an infinite key) has no weight; where all are, the result is zeros.
  */
 int videomla_paged_attend(const videomla_dims* dims, const videomla_paged* paged,
                           const uint16_t* q_nope, const uint16_t* q_r, const uint16_t* w_uk,

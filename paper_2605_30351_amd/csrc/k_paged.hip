@@ -92,8 +92,9 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
   int left = wk.n, blk = wk.block, end = wk.end;
 
   // Load j of a tile fills the chunk slots 64 j .. 64 j + 63: of this lane's chunk, in bits 0..15 the
-  // offset in its row's c_kv, or (bit 31) k_r (the pad reads k_r again, against zeros in q_cat), in bits
-  // 16..19 the row modulo 16. Half a tile is a whole number of loads, and the other half repeats it.
+  // offset in its row's c_kv, or (bit 31) k_r, or (bit 30) the pad of q_cat's first row, which is zero as the
+  // pad has to be (an infinity there, times the zero in q_cat, would be NaN); in bits 16..19 the row modulo
+  // 16. Half a tile is a whole number of loads, and the other half repeats it.
   // (SPLIT: of the two loads of k_r, from load 32 on.)
   constexpr int NAT = C::SPLIT ? 1 : C::NDMA / 2;
   uint32_t d_at[NAT];
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
 #pragma unroll
     for (int j = 0; j < NAT; ++j) {
       const int slot = j * 64 + lane, r = slot / C::CPR, c = (slot % C::CPR) ^ C::swz(r);
-      d_at[j] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : 0x80000000u | (c < (DC + DR) / 8 ? c * 8 - DC : 0));
+      d_at[j] = (uint32_t)r << 16 | (c < DC / 8 ? c * 8 : c < (DC + DR) / 8 ? 0x80000000u | (c * 8 - DC) : 0x40000000u);
     }
   }
 
@@ -198,7 +199,9 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
         const uint32_t r = __shfl(at_row, (int)(at >> 16 & 15) + 16 * half);
         const bool kr = (int32_t)at < 0;
         const uint16_t* p = (kr ? a.k_r : a.c_kv) + (at & 0xffffu);
-        lds_dma16(p + (uint64_t)r * (uint32_t)(kr ? DR : DC), lds + 1024u * j);
+        p += (uint64_t)r * (uint32_t)(kr ? DR : DC);
+        if constexpr (C::DQKP > DC + DR) p = at & 0x40000000u ? a.qcat + DC + DR : p;
+        lds_dma16(p, lds + 1024u * j);
       }
     };
 
@@ -244,10 +247,11 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
       // Both terms of the absorbed queries: one alone is off by up to 2^-8 of each component, which moves a
       // score of size |s| by about 2^-9.5 |s| and weighs most where the softmax is peaked (scores of standard
       // deviation 4: outputs off by 0.0044 in the 2-norm with one term, 0.0018 with two). These matrix steps
-      // pass under the loads of the keys, which bound this kernel.
-      f32x4 s[QB][2];
+      // pass under the loads of the keys, which bound this kernel. The second term's sum is kept apart: of an
+      // infinite k^R the two may be infinities of opposite signs, and the first alone is the score.
+      f32x4 s[QB][2], s_lo[QB][2];
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{};
+      for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = s_lo[qb][0] = s_lo[qb][1] = f32x4{};
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
         const bf16x8 k0v = as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[k_at(0, ks)]));
@@ -260,10 +264,14 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
           bf16x8 ql;
           if constexpr (C::LO_REG) ql = qlo[qb][ks];
           else ql = q_at(1, qb, ks);
-          s[qb][0] = mfma16(k0v, ql, s[qb][0]);
-          s[qb][1] = mfma16(k1v, ql, s[qb][1]);
+          s_lo[qb][0] = mfma16(k0v, ql, s_lo[qb][0]);
+          s_lo[qb][1] = mfma16(k1v, ql, s_lo[qb][1]);
         }
       }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[qb][i >> 2][i & 3] += second_or_zero(s_lo[qb][i >> 2][i & 3]);
       if (masked) {
         float least = s[0][0][0];
 #pragma unroll

@@ -62,18 +62,20 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   int left = wk.n, blk = wk.block, end = wk.end;
   if (threadIdx.x == 0) cleared = 0;
 
-  // this wave's loads j = wave + NW i of a tile: where this lane's chunk is in pool row 0 of c_kv, or of k_r
-  // (the pad reads k_r again, against zeros in q_cat); the tile row, and the bytes of a pool row
+  // this wave's loads j = wave + NW i of a tile: where this lane's chunk is in pool row 0 of c_kv, or of k_r, or
+  // (the pad, which has to be zero: times the zero in q_cat an infinity would be NaN) in the pad of q_cat's
+  // first row; the tile row, and the bytes of a pool row
   const uint16_t* d_src[C::PER_WAVE];
   int d_row[C::PER_WAVE];
-  bool d_kr[C::PER_WAVE];
+  bool d_kr[C::PER_WAVE], d_pad[C::PER_WAVE];
 #pragma unroll
   for (int i = 0; i < C::PER_WAVE; ++i) {
     const int j = wave + NW * i, slot = (j < C::NDMA ? j : 0) * 64 + lane;
     const int r = slot / C::CPR, c = C::pos(r, slot % C::CPR);
     d_row[i] = r;
     d_kr[i] = c >= DC / 8;
-    d_src[i] = c < DC / 8 ? a.c_kv + c * 8 : a.k_r + (c < (DC + DR) / 8 ? c * 8 - DC : 0);
+    d_pad[i] = c >= (DC + DR) / 8;  // (never at most widths)
+    d_src[i] = c < DC / 8 ? a.c_kv + c * 8 : d_pad[i] ? a.qcat + DC + DR : a.k_r + (c * 8 - DC);
   }
   // K operand of step ks: row l32, chunk 2 ks + g; V^T transpose reads: rows 4 g + tr_row (+ 8), columns
   // tr_col (+ 32 d, + 16 rows per half)
@@ -108,7 +110,10 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     uint32_t from[C::PER_WAVE];  // the pool rows of this lane's chunks (a missing key stages the first row)
     auto rows_for = [&](int row) {
 #pragma unroll
-      for (int i = 0; i < C::PER_WAVE; ++i) from[i] = __shfl(max(row, 0), d_row[i]);
+      for (int i = 0; i < C::PER_WAVE; ++i) {
+        from[i] = __shfl(max(row, 0), d_row[i]);
+        if constexpr (C::DQKP > DC + DR) from[i] = d_pad[i] ? 0 : from[i];
+      }
     };
     auto load_part = [&](int i, uint16_t* buf) {
       const int j = wave + NW * i;
@@ -234,6 +239,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
                    as_bf16x8(*reinterpret_cast<const u32x4*>(own + ks * 512)), s);
         if (ks & 1) __builtin_amdgcn_sched_barrier(0);  // (all reads at once would not fit the registers)
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = second_or_zero(s[r]);
     };
 
     // One step: scores of tile t + 1 (QK), the exponentials of tile t (SM) and O += V^T P^T of tile t (PV)

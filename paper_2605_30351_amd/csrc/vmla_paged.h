@@ -146,6 +146,10 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kMasked = -__builtin_huge_valf();
 constexpr float kLazyMaxStep = 8.0f;  // the running max is raised when exceeded by more (log2 units)
 
+// The second query term's part of a score, where it is finite: of an infinite key it is an infinity too, whose
+// sign may be the opposite of the first term's, which alone is the score then.
+__device__ __forceinline__ float second_or_zero(float v) { return fabsf(v) < __builtin_huge_valf() ? v : 0.f; }
+
 // Of 32 keys, those of the bit set `keys` in [b, e).
 __device__ __forceinline__ uint32_t seen_keys(uint32_t keys, int b, int e) {
   const int lo = min(max(b, 0), 32), hi = min(max(e, 0), 32);

@@ -1,6 +1,8 @@
 """Paged attention with infinities in tokens that queries do see: the result is the definition's, wherever
 mask, window and tile boundaries fall. An infinite latent makes a score of plus or minus infinity (or NaN,
-with several) and a value that is not finite, so that 0 * inf or inf - inf is left whatever its sign: NaN."""
+with several) and a value that is not finite, so that 0 * inf or inf - inf is left whatever its sign: NaN. An
+infinite rotated key has a finite value: at plus infinity the row is NaN, at minus infinity the key has no
+weight, as if it were hidden."""
 import numpy as np
 import pytest
 
@@ -10,7 +12,7 @@ ensure_built()
 
 import paper_2605_30351_amd  # noqa: E402, F401
 from tests.gpu_common import bf16_to_f64, host_bits  # noqa: E402
-from tests.paged_common import Batch, assert_within  # noqa: E402
+from tests.paged_common import Batch, assert_within, rope  # noqa: E402
 from tests.test_gpu_paged import TEXT, attend  # noqa: E402
 from workloads import TINY  # noqa: E402
 
@@ -21,8 +23,18 @@ IDS = [f"dc{d.d_c}" for d in WIDTHS]
 INF, NEG = 0x7f80, 0xff80
 
 
-def batch(dims, max_new, mask, window):
-    return Batch(dims, [(40, 150, 3), (1, 70, 0)], page=20, mask=mask, window=window, seed=41, max_new=max_new)
+class Without(Batch):
+    """A batch whose queries do not see cached token `gone` of sequence 0."""
+    gone = -1
+
+    def seen(self, s, i):
+        return [j for j in super().seen(s, i) if s or j != self.gone]
+
+
+def batch(dims, max_new, mask, window, gone=-1, gain=1.0):
+    b = Without(dims, [(40, 150, 3), (1, 70, 0)], page=20, mask=mask, window=window, seed=41, max_new=max_new, gain=gain)
+    b.gone = gone
+    return b
 
 
 def seers(b, j):
@@ -50,3 +62,24 @@ def test_an_infinite_latent_reaches_every_query_that_sees_it(dims, max_new, j):
             assert np.isnan(got[see]).all(), (label, int(np.isfinite(got[see]).sum()))
             keep = np.setdiff1d(np.arange(b.rows), see)
             assert_within(got[keep], want[keep], bound[keep], label)
+
+
+@pytest.mark.parametrize("j", [5, 121, 149])
+@pytest.mark.parametrize("max_new,gain", [(1, 1.0), (40, 1.0), (40, 4.0)])
+@pytest.mark.parametrize("dims", WIDTHS, ids=IDS)
+def test_an_infinite_key_is_seen_by_the_sign_of_its_score(dims, max_new, gain, j):
+    for mask, window in ((1, 0), (16, 60)):
+        b, without = (batch(dims, max_new, mask, window, gone, gain) for gone in (-1, j))
+        (want, bound), (want_gone, bound_gone) = b.attention(), without.attention()
+        b.k_r.reshape(-1, dims.d_rope)[b.pool_row(0, j), 0] = INF
+        got = bf16_to_f64(host_bits(attend(b)))
+        see = seers(b, j)
+        q = rope(dims, bf16_to_f64(b.q_r[see]), (3 + 110 + see)[:, None])[..., 0]
+        for n, i in enumerate(see):
+            for h in range(dims.n_heads):
+                if q[n, h] > 0:
+                    want[i, h] = np.nan
+                    assert np.isnan(got[i, h]).all(), (dims.d_c, j, mask, i, h)
+                else:
+                    want[i, h], bound[i, h] = want_gone[i, h], bound_gone[i, h]
+        assert_within(got, want, bound, f"{dims.d_c} key {j} mask {mask} window {window}")
