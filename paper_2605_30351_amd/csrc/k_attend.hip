@@ -164,16 +164,30 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
     }
     if (c0 == 0) VMLA_STAMP(a, kStampQAbsorb, 2);
     if (STAGE) __syncthreads();  // every wave is done reading W_UK_h: its area holds the rows
-    [[maybe_unused]] bool with_lo = ok;  // this token's second terms are wanted
+    float scale = a.qscale;
+    auto scaled = [&](int cb, int i) {
+      return f32x4{acc[cb][4 * i] * scale, acc[cb][4 * i + 1] * scale, acc[cb][4 * i + 2] * scale,
+                   acc[cb][4 * i + 3] * scale};
+    };
     if constexpr (PAGED && STAGE) {
-      if (a.unit == 32) {
-        float n2 = 0.f;
+      if (a.q_low) {  // the 8 further bits pass through the wave's tile before the first terms
+        uint8_t* ob = reinterpret_cast<uint8_t*>(ot);
+        constexpr int BS = DC + 16;  // row stride (bytes)
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (cb * 32 + 8 * (i >> 2) < DC) n2 += acc[cb][i] * acc[cb][i];
-        with_lo = ok && half_swap_sum(n2) * a.qscale * a.qscale > 0.9f * kOneTerm * kOneTerm;
+          for (int i = 0; i < 4; ++i) {
+            const int c = cb * 32 + 8 * i + 4 * g;
+            if (c < DC) *reinterpret_cast<uint32_t*>(ob + l32 * BS + c) = low_bits_of(scaled(cb, i));
+          }
+#pragma unroll 4
+        for (int i = lane; i < 32 * (DC / 16); i += 64) {
+          const int t = i / (DC / 16), k = i - t * (DC / 16);
+          if (tok0 + t < Nq)
+            *reinterpret_cast<u32x4*>(a.q_low + ((int64_t)(tok0 + t) * H + h) * DQKP + k * 16) =
+                *reinterpret_cast<const u32x4*>(ob + t * BS + k * 16);
+        }
+        asm volatile("" : "+s"(scale));  // the products are taken again: kept, they would cost a wave per SIMD
       }
     }
     if (ok || STAGE) {
@@ -183,11 +197,10 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
         for (int i = 0; i < 4; ++i) {
           const int c = c0 + cb * 32 + 8 * i + 4 * g;
           if (c < DC) {
-            const f32x4 v = {acc[cb][4 * i] * a.qscale, acc[cb][4 * i + 1] * a.qscale,
-                             acc[cb][4 * i + 2] * a.qscale, acc[cb][4 * i + 3] * a.qscale};
+            const f32x4 v = scaled(cb, i);
             *reinterpret_cast<bf16x4*>(STAGE ? ot + l32 * OS + c : dst + c) = to_bf16x4(v);
             if constexpr (PAGED) {
-              if (with_lo) paged_q_lo(a, (int64_t)row * DQKP + c, v);
+              if (ok && (!STAGE || a.q_lo)) paged_q_lo(a, (int64_t)row * DQKP + c, v);
             }
           }
         }
@@ -202,7 +215,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
     float u = bf16_bits_to_f32((uint16_t)(raw & 0xffff)), v = bf16_bits_to_f32((uint16_t)(raw >> 16));
     rotate_by(rope_cos_sin_at(qpos[wave][rp.axis][t - tok0], rp.theta), u, v);
     if constexpr (PAGED) {
-      if (a.q_lo) paged_q_pair(a, (int64_t)r * DQKP + DC + 2 * p, u * a.qscale, v * a.qscale);
+      if (a.q_lo || a.q_low) paged_q_pair(a, (int64_t)r * DQKP + DC + 2 * p, u * a.qscale, v * a.qscale);
     }
     const uint32_t packed =
         (uint32_t)to_bf16_bits(u * a.qscale) | ((uint32_t)to_bf16_bits(v * a.qscale) << 16);
@@ -234,6 +247,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
         else a.qcat[r * DQKP + c] = 0;
         if constexpr (PAGED) {
           if (a.q_lo) a.q_lo[r * DQKP + c] = 0;
+          if (a.q_low) a.q_low[r * DQKP + c] = 0;
         }
       }
     }

@@ -268,10 +268,11 @@ __global__ __launch_bounds__(64 * few_waves(DC)) void paged_attend_few_kernel(co
           s_lo[qb][1] = mfma16(k1v, ql, s_lo[qb][1]);
         }
       }
+      const float most = most_here();
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[qb][i >> 2][i & 3] += second_or_zero(s_lo[qb][i >> 2][i & 3]);
+        for (int i = 0; i < 8; ++i) s[qb][i >> 2][i & 3] += second_part(s_lo[qb][i >> 2][i & 3], most);
       if (masked) {
         float least = s[0][0][0];
 #pragma unroll

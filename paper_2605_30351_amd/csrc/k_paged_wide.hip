@@ -13,11 +13,12 @@
 // key hidden from a row has probability 0 there, and 0 * NaN would reach it. The same holds for missing
 // keys (holes, keys past the end), in whose place the pool's first row is staged.
 //
-// Queries are multiplied as one bf16 term (14 of the 26 matrix steps of a tile at d_c = 192) while they are
-// short: the rounding moves a score by about 2^-9.5 of its size, and so the output by 0.0016 in the 2-norm
-// at scores of standard deviation 1, beside 0.0017 of the output's own rounding, and in proportion beyond.
-// A wave with an absorbed query longer than kOneTerm adds the second terms of such queries, from LDS, before
-// the first: its tile takes about 1.5 times as long.
+// Queries are multiplied as one bf16 term (14 of the 26 matrix steps of a tile at d_c = 192) while scores are small:
+// the rounding moves a score by about 2^-9.5 of its size, and so the output by 0.0016 in the 2-norm at scores of
+// standard deviation 1, beside 0.0017 of the output's own rounding, and in proportion beyond. A workgroup's part
+// of a block that needs it (kOneTerm, kSpread) is multiplied with both terms, the second from LDS before the first:
+// a tile takes about 1.5 times as long. Looking for it costs 1% at most: it is done in the first tile and where a
+// running maximum is raised (a look at every tile cost 4 to 10%).
 #include <type_traits>
 
 #include "vmla_paged.h"
@@ -51,6 +52,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   __shared__ __attribute__((aligned(16))) uint16_t tile[3][C::TILE];
   __shared__ __attribute__((aligned(16))) uint16_t q_lo[NW][C::KS][64 * 8];  // each wave's second term, by lane
   __shared__ uint32_t cleared;  // keys of the tile in work, between settle()'s barriers
+  __shared__ int two_terms;     // the segment is to be taken with two terms: by its rows, or its first tile's scores
+  __shared__ int far[2];        // its later scores are far apart (segments in turn)
   __shared__ __attribute__((aligned(16))) float resc[C::RESC_LDS ? NW : 1][C::RESC_LDS ? 64 * 16 : 4];
 
   const int lane = threadIdx.x & 63;
@@ -85,7 +88,23 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
   const int tr_row = (lane & 15) >> 2, tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   const int vofs_lo = C::at(4 * g + tr_row, tr_col), vofs_hi = C::at(4 * g + tr_row + 8, tr_col);
 
-  while (left > 0) {
+  // A part whose later scores were too far apart for one term is taken again, with two: the waves agree on that at
+  // the barrier that the next part begins with, so that its results, wrong then, are written without a wait.
+  bool again = false, one_term = false;
+  int left0 = 0, blk0 = 0, end0 = 0, turn = 0;
+  for (;;) {
+    __syncthreads();  // the previous segment's tiles are no longer read
+    again = one_term && __builtin_amdgcn_readfirstlane(far[turn]) != 0;
+    if (again) {
+      left = left0;
+      blk = blk0;
+      end = end0;
+    }
+    one_term = false;
+    if (left <= 0) break;
+    left0 = left;
+    blk0 = blk;
+    end0 = end;
     const bool last = blk == wk.block;  // (whose record the plan has copied: one load less in line)
     const PagedBlock pb = last ? paged_read<true>(a.plan.work_block, blockIdx.x) : paged_read<true>(a.plan.block, blk);
     if (end < 0) end = pb.n_units + a.cost;  // a block before the workgroup's last is taken to its end
@@ -97,7 +116,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     const int row0 = pb.row0 + wave * 32, n_rows = pb.n_rows;
     const int key0 = pb.key0 + u0 * 32;
     const int32_t* table = pg.table + (int64_t)pb.seq * pg.max_pages;
-    __syncthreads();  // the previous segment's tiles are no longer read
+    turn ^= 1;
+    if (threadIdx.x == 0) two_terms = far[turn] = 0;
 
     // page ids of tile t's keys, one per lane (a key outside the sequence reads the nearest entry)
     auto load_id = [&](int t) { return table[page_of(pg, min(key0 + t * 32 + l32, pg.max_kv - 1))]; };
@@ -142,9 +162,8 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     int see_b, see_e;
     const int r_own = row0 + l32;
     const bool live = r_own < n_rows;
-    const int64_t q_at = ((int64_t)pb.lo * H + (live ? r_own : 0)) * C::DQKP + 8 * g;
     {
-      const uint16_t* src = a.qcat + q_at;
+      const uint16_t* src = a.qcat + ((int64_t)pb.lo * H + (live ? r_own : 0)) * C::DQKP + 8 * g;
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
         u32x4 v = ldg16(src + ks * 16);
@@ -177,11 +196,21 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       if (seen_keys(keys, see_b - k0, see_e - k0) & cleared_keys(&cleared)) spoiled = kNotANumber;
     };
 
-    auto masked_tile = [&](uint32_t keys, int k0) { return keys != 0xffffffffu || k0 < b_max || k0 + 32 > e_min; };
-    auto mask = [&](f32x16& s, uint32_t keys, int k0) {
+    auto mask = [&](f32x16& s, uint32_t keys, int t) {
+      const int k0 = key0 + t * 32;
+      if (keys == 0xffffffffu && k0 >= b_max && k0 + 32 <= e_min) return;
       const uint32_t seen = seen_keys(keys, see_b - k0, see_e - k0) >> (4 * g);
+      const float masked = __uint_as_float(bits_here<0xff800000u>());  // kMasked
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = seen >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : kMasked;
+      for (int r = 0; r < 16; ++r) s[r] = seen >> (8 * (r >> 2) + (r & 3)) & 1 ? s[r] : masked;
+    };
+    // Whether some row's scores (masked) are further apart than kSpread. Of four differences a lane, of keys 1, 8, 10
+    // and 16 apart, two have to be, so that a single key that stands out does not count.
+    auto apart = [&](const f32x16& s) {
+      f32x4 d = {fabsf(s[0] - s[1]), fabsf(s[2] - s[6]), fabsf(s[4] - s[12]), fabsf(s[9] - s[15])};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d[i] = d[i] < -kMasked ? d[i] : 0.f;  // (a hidden key's is infinite, or NaN)
+      return __builtin_amdgcn_ballot_w64(fminf(fmaxf(d[0], d[1]), fmaxf(d[2], d[3])) > kSpread) != 0;
     };
     auto max_of = [&](const f32x16& v) {  // a tree of three-input maxima
       const float a0 = fmaxf(fmaxf(v[0], v[1]), v[2]), a1 = fmaxf(fmaxf(v[3], v[4]), v[5]);
@@ -190,8 +219,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       return fmaxf(fmaxf(fmaxf(a0, a1), a2), fmaxf(fmaxf(a3, a4), v[15]));
     };
     // each lane sees half of its row's keys; growth on either half sends the wave through the rare path
-    auto raise_max = [&]() {
+    auto raise_max = [&](const f32x16& s, auto both) {
       if (__builtin_amdgcn_ballot_w64(own_max > m_run + kLazyMaxStep) == 0) return;
+      if (!decltype(both)::value && apart(s)) far[turn] = 1;
       const float m_new = fmaxf(m_run, half_swap_max(own_max));
       const float alpha = fast_exp2(m_run - m_new);
       m_run = m_new;
@@ -213,25 +243,26 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       }
     };
 
-    float q2 = 0.f;  // the squared length of this lane's absorbed query
+    float q2 = 0.f;  // the squared length of this lane's query
 #pragma unroll
-    for (int ks = 0; ks < DC / 16; ++ks) {
+    for (int ks = 0; ks < C::KS; ++ks) {
       const bf16x2 h[4] = {__builtin_shufflevector(q[ks], q[ks], 0, 1), __builtin_shufflevector(q[ks], q[ks], 2, 3),
                            __builtin_shufflevector(q[ks], q[ks], 4, 5), __builtin_shufflevector(q[ks], q[ks], 6, 7)};
 #pragma unroll
       for (int i = 0; i < 4; ++i) q2 = __builtin_amdgcn_fdot2_f32_bf16(h[i], h[i], q2, false);
     }
-    const bool is_long = live && half_swap_sum(q2) > kOneTerm * kOneTerm;
-    const bool two = __builtin_amdgcn_ballot_w64(is_long) != 0;
-    if (two) {
+    const bool long_row = __builtin_amdgcn_ballot_w64(half_swap_sum(q2) > kOneTerm * kOneTerm) != 0;
+    auto fetch_lo = [&]() {
+      const int ln = lane_here(), r = row0 + (ln & 31);
+      const uint8_t* src = a.q_low + ((int64_t)pb.lo * H + (r < n_rows ? r : 0)) * C::DQKP + 8 * (ln >> 5);
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
-        u32x4 v = ldg16(a.q_lo + q_at + ks * 16);
-        if (!is_long) v = u32x4{0, 0, 0, 0};  // (not written)
-        *reinterpret_cast<u32x4*>(&q_lo[wave][ks][lane * 8]) = v;
+        u32x2 v = *reinterpret_cast<const u32x2*>(src + ks * 16);
+        if (r >= n_rows) v = u32x2{0, 0};
+        *reinterpret_cast<bf16x8*>(&q_lo[wave][ks][ln * 8]) = second_term(q[ks], v);
       }
-    }
-    auto second_term = [&](const uint16_t* buf, f32x16& s) __attribute__((always_inline)) {
+    };
+    auto add_low = [&](const uint16_t* buf, f32x16& s) __attribute__((always_inline)) {
       const uint16_t* own = &q_lo[wave][0][lane_here() * 8];
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks) {
@@ -239,8 +270,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
                    as_bf16x8(*reinterpret_cast<const u32x4*>(own + ks * 512)), s);
         if (ks & 1) __builtin_amdgcn_sched_barrier(0);  // (all reads at once would not fit the registers)
       }
+      const float most = most_here();
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = second_or_zero(s[r]);
+      for (int r = 0; r < 16; ++r) s[r] = second_part(s[r], most);
     };
 
     // One step: scores of tile t + 1 (QK), the exponentials of tile t (SM) and O += V^T P^T of tile t (PV)
@@ -272,7 +304,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
         pk[p] = __builtin_bit_cast(uint32_t, h);
       };
       f32x16 acc = {};
-      if constexpr (decltype(two_terms)::value) second_term(nxt, acc);
+      if constexpr (decltype(two_terms)::value) add_low(nxt, acc);
       bf16x8 kq[3], vq[2];
       kq[0] = kread(0);
       if (NS > 1) kq[1] = kread(1);
@@ -304,9 +336,9 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       wait_vmcnt<0>();  // this wave's part of tile t + 2 is in LDS
       __syncthreads();
       settle(t + 1, keys, nxt);
-      if (masked_tile(keys, key0 + (t + 1) * 32)) mask(s_nxt, keys, key0 + (t + 1) * 32);
+      mask(s_nxt, keys, t + 1);
       own_max = max_of(s_nxt);
-      raise_max();
+      raise_max(s_nxt, two_terms);
     };
 
     wait_vmcnt<0>();
@@ -314,6 +346,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
     if (row0 >= n_rows) {  // no rows: this wave only loads
       __syncthreads();
       settle(0, there, tile[0]);
+      one_term = !again && __builtin_amdgcn_readfirstlane(two_terms) == 0;
       int fill = 2;
       for (int t = 0; t < n_tiles; ++t) {
         row = row_of(t + 2, id);
@@ -328,31 +361,38 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
       }
     } else {
       f32x16 s_a = {}, s_b;
-      if (two) second_term(tile[0], s_a);
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks)
         s_a = mfma32(as_bf16x8(*reinterpret_cast<const u32x4*>(&tile[0][((ks & 1) ? koff_o : koff_e) + ks * 16])),
                      q[ks], s_a);
+      mask(s_a, there, 0);
+      if (long_row || apart(s_a)) two_terms = 1;
       __syncthreads();  // every wave has used tile 0's K
       settle(0, there, tile[0]);
-      if (masked_tile(there, key0)) mask(s_a, there, key0);
+      one_term = !again && __builtin_amdgcn_readfirstlane(two_terms) == 0;
+      if (!one_term) {  // (K is as it was, but for what makes a row NaN)
+        fetch_lo();
+        s_b = f32x16{};
+        add_low(tile[0], s_b);
+        s_a += s_b;
+      }
       own_max = max_of(s_a);
       m_run = fmaxf(kLowest, half_swap_max(own_max));  // nothing to rescale yet
-      auto steps = [&](auto two_terms) __attribute__((always_inline)) {
+      auto steps = [&](auto both) __attribute__((always_inline)) {
         uint16_t *pc = tile[0], *pn = tile[1], *ps = tile[2];  // tile t lives in buffer t mod 3
         int t = 0;
         for (; t + 1 < n_tiles; t += 2) {
-          step(t, s_a, s_b, pc, pn, ps, two_terms);
-          step(t + 1, s_b, s_a, pn, ps, pc, two_terms);
+          step(t, s_a, s_b, pc, pn, ps, both);
+          step(t + 1, s_b, s_a, pn, ps, pc, both);
           uint16_t* tmp = pc;
           pc = ps;
           ps = pn;
           pn = tmp;
         }
-        if (t < n_tiles) step(t, s_a, s_b, pc, pn, ps, two_terms);
+        if (t < n_tiles) step(t, s_a, s_b, pc, pn, ps, both);
       };
-      if (two) steps(std::true_type{});
-      else steps(std::false_type{});
+      if (one_term) steps(std::false_type{});
+      else steps(std::true_type{});
 
       // ---- a whole block's latents, or this segment's partial result ----
       const float l = half_swap_sum(l_run + spoiled);

@@ -130,6 +130,15 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// A constant of these bits, put into its register where it is used: out of the loops, where the compiler moves
+// constants that no instruction can hold, it would keep a register that is not there.
+template <uint32_t BITS>
+__device__ __forceinline__ uint32_t bits_here() {
+  uint32_t v;
+  asm volatile("v_mov_b32 %0, %1" : "=v"(v) : "n"(BITS));
+  return v;
+}
+
 // Direct global-to-LDS load of 16 B per lane (see lds_dma16) from a scalar base and a lane offset in bytes.
 // The base has to be settled (no VALU instruction may write it in the five wait states before): callers
 // compute it with scalar arithmetic.
@@ -146,9 +155,10 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kMasked = -__builtin_huge_valf();
 constexpr float kLazyMaxStep = 8.0f;  // the running max is raised when exceeded by more (log2 units)
 
-// The second query term's part of a score, where it is finite: of an infinite key it is an infinity too, whose
-// sign may be the opposite of the first term's, which alone is the score then.
-__device__ __forceinline__ float second_or_zero(float v) { return fabsf(v) < __builtin_huge_valf() ? v : 0.f; }
+// The second query term's part of a score, made finite: of an infinite key it is an infinity too, whose sign may
+// be the opposite of the first term's, which alone is the score then.
+__device__ __forceinline__ float second_part(float v, float most) { return __builtin_amdgcn_fmed3f(v, kLowest, most); }
+__device__ __forceinline__ float most_here() { return __uint_as_float(bits_here<0x7f7fffffu>()); }
 
 // Of 32 keys, those of the bit set `keys` in [b, e).
 __device__ __forceinline__ uint32_t seen_keys(uint32_t keys, int b, int e) {
@@ -162,6 +172,8 @@ __device__ __forceinline__ int lane_here() {
   asm volatile("" : "+s"(zero));
   return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
 }
+
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
 
 // bf16 values with infinities and NaN replaced by zero. In a tile that is masked for some row, a key's
 // probability may be 0 while its latent is not finite, and 0 * NaN would reach the rows that do not see
@@ -181,7 +193,7 @@ __device__ __forceinline__ bool not_finite(u32x4 u) {
   const uint32_t e = 0x7f807f80u, one = 0x00800080u;
   return (((u[0] & e) + one | (u[1] & e) + one | (u[2] & e) + one | (u[3] & e) + one) & 0x80008000u) != 0;
 }
-constexpr float kNotANumber = __builtin_nanf("");
+#define kNotANumber __uint_as_float(0xffffffffu)  // (an inline constant of the instructions, which 0x7fc00000 is not)
 
 // Of a tile's 32 keys those whose latents are not all finite; chunk_at(key, c): where 8 of them are. For waves
 // that clear the latents in registers, called where some score is minus infinity, as it is with such a latent
@@ -213,10 +225,13 @@ __device__ __forceinline__ void clear_not_finite(uint16_t* p, uint32_t* word, Ke
 // have a barrier between two rounds.
 __device__ __forceinline__ uint32_t cleared_keys(uint32_t* word) {
   __syncthreads();
-  const uint32_t keys = __builtin_amdgcn_readfirstlane(*word);
+  uint32_t at = lds_addr(word);
+  asm volatile("" : "+v"(at));  // (see bits_here)
+  volatile lds_u32* const here = (volatile lds_u32*)(at);
+  const uint32_t keys = __builtin_amdgcn_readfirstlane(*here);
   if (keys != 0) {
     __syncthreads();  // every wave has read it
-    if (threadIdx.x == 0) *word = 0;
+    if (threadIdx.x == 0) *here = 0;
   }
   return keys;
 }
@@ -291,30 +306,65 @@ struct PagedWriteArgs : WriteArgs {
 struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
-  uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), or nullptr (512-wide kernel)
+  uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), for the few-row kernel, or nullptr
+  uint8_t* q_low;      // workspace: the same in 8 bits (low_bits_of), for the wide kernel, or nullptr
   float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
   int32_t cost;        // counts of a block beyond its units
 };
 
-// The wide kernel takes the second term of rows whose latent part of q_cat is longer than this, in exponents
-// of 2 (against latents of unit RMS: a standard deviation of the scores); the absorption writes it for these
-// and, as it compares before the rounding, for those just below.
-constexpr float kOneTerm = 2.3f;
+// The wide kernel multiplies the second term of q_cat where one alone would be off by more than about the output's
+// own rounding: where a block has a row longer than kOneTerm (against keys of unit RMS: the standard deviation of
+// its scores, in exponents of 2) and, of whatever scale queries and keys are, where the scores of some row are
+// further apart than kSpread in the first tile of a workgroup's part of a block, or in a later one that raises a
+// running maximum, as those of larger keys do: then it takes its part again from the start. Of 256 rows one is
+// found in the first tile if their deviation is 3 or more; at 1.4, of a plain softmax over unit vectors, none in
+// 10^6 tiles is.
+constexpr float kOneTerm = 2.3f, kSpread = 10.f;
 
-// The second bf16 term of four values of q_cat (their first has been, or is, rounded from them), where the
-// call keeps one; both terms of a pair.
-__device__ __forceinline__ void paged_q_lo(const PagedAttendArgs& a, int64_t at, f32x4 v) {
-  if (a.q_lo)
-    *reinterpret_cast<bf16x4*>(a.q_lo + at) = to_bf16x4(v - __builtin_convertvector(to_bf16x4(v), f32x4));
+// The second bf16 term of four values of q_cat (their first has been, or is, rounded from them). The few-row
+// kernel reads it as it is. For the wide kernel, which seldom does, the absorption writes half the bytes: the
+// 8 bits of the value that follow its first term's, as the signed distance from it in steps of the float's bit
+// pattern (of 2^-8 of the first term's last place).
+__device__ __forceinline__ bf16x4 second_term_of(f32x4 v) {
+  return to_bf16x4(v - __builtin_convertvector(to_bf16x4(v), f32x4));
 }
+__device__ __forceinline__ uint32_t low_bits(float v, uint32_t first) {  // in bits 8 .. 15
+  return (uint32_t)min((int)(__float_as_uint(v) - (first << 16)), 0x7fff);
+}
+__device__ __forceinline__ uint32_t low_bits_of(f32x4 v) {
+  const u32x2 h = __builtin_bit_cast(u32x2, to_bf16x4(v));
+  const uint32_t l01 = __builtin_amdgcn_perm(low_bits(v[1], h[0] >> 16), low_bits(v[0], h[0] & 0xffffu), 0x0c0c0501u);
+  const uint32_t l23 = __builtin_amdgcn_perm(low_bits(v[3], h[1] >> 16), low_bits(v[2], h[1] & 0xffffu), 0x0c0c0501u);
+  return l01 | l23 << 16;
+}
+// The second term from the first and those bits (exact: it has at most 8).
+__device__ __forceinline__ bf16x8 second_term(bf16x8 first, u32x2 low) {
+  const u32x4 h = as_u32x4(first);
+  f32x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t hi = i & 1 ? h[i >> 1] & 0xffff0000u : h[i >> 1] << 16;
+    const int32_t lo = (int32_t)(low[i >> 2] << (24 - 8 * (i & 3))) >> 24;
+    v[i] = __uint_as_float(hi + ((uint32_t)lo << 8)) - __uint_as_float(hi);
+  }
+  return to_bf16x8(v);
+}
+__device__ __forceinline__ void paged_q_lo(const PagedAttendArgs& a, int64_t at, f32x4 v) {
+  if (a.q_lo) *reinterpret_cast<bf16x4*>(a.q_lo + at) = second_term_of(v);
+  if (a.q_low) *reinterpret_cast<uint32_t*>(a.q_low + at) = low_bits_of(v);
+}
+// Both terms of a pair.
 __device__ __forceinline__ void paged_q_pair(const PagedAttendArgs& a, int64_t at, float u, float v) {
   const uint16_t hu = to_bf16_bits(u), hv = to_bf16_bits(v);
   *reinterpret_cast<uint32_t*>(a.qcat + at) = (uint32_t)hu | (uint32_t)hv << 16;
   if (a.q_lo)
     *reinterpret_cast<uint32_t*>(a.q_lo + at) = (uint32_t)to_bf16_bits(u - bf16_bits_to_f32(hu)) |
                                                 (uint32_t)to_bf16_bits(v - bf16_bits_to_f32(hv)) << 16;
+  if (a.q_low)
+    *reinterpret_cast<uint16_t*>(a.q_low + at) =
+        (uint16_t)__builtin_amdgcn_perm(low_bits(v, hv), low_bits(u, hu), 0x0c0c0501u);
 }
 
 constexpr int kPagedMaxSeqs = 4096;
