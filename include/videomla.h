@@ -476,9 +476,8 @@ size_t videomla_paged_attend_workspace_bytes(const videomla_dims* dims, const vi
  *   workspace  device buffer of at least videomla_paged_attend_workspace_bytes() bytes; every call
  *              writes what it reads there, so that calls ordered on one stream may share one
  * Arithmetic, shapes and errors of videomla_attend, but for the absorbed queries: they are multiplied as
- * two bf16 terms in calls of few rows per sequence and, up to d_c = 256, wherever one is long or its scores
- * are far apart, of whatever scale queries and latents are. Results are
- * bitwise reproducible. Infinities and NaN in tokens that a query does not see do not reach it; in the
+ * two bf16 terms in calls of few rows per sequence, and wherever one is long or its scores are far apart, of
+ * whatever scale queries and latents are. Results are bitwise reproducible. Infinities and NaN in tokens that a query does not see do not reach it; in the
  * latents of a token that it sees they make its result NaN, as 0 * inf and inf - inf do. A token whose
  * score is minus infinity (of an infinite key) has no weight; where all are, the result is zeros.
  */

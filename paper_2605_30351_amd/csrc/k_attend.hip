@@ -164,30 +164,22 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
     }
     if (c0 == 0) VMLA_STAMP(a, kStampQAbsorb, 2);
     if (STAGE) __syncthreads();  // every wave is done reading W_UK_h: its area holds the rows
-    float scale = a.qscale;
     auto scaled = [&](int cb, int i) {
-      return f32x4{acc[cb][4 * i] * scale, acc[cb][4 * i + 1] * scale, acc[cb][4 * i + 2] * scale,
-                   acc[cb][4 * i + 3] * scale};
+      return f32x4{acc[cb][4 * i] * a.qscale, acc[cb][4 * i + 1] * a.qscale, acc[cb][4 * i + 2] * a.qscale,
+                   acc[cb][4 * i + 3] * a.qscale};
     };
-    if constexpr (PAGED && STAGE) {
-      if (a.q_low) {  // the 8 further bits pass through the wave's tile before the first terms
-        uint8_t* ob = reinterpret_cast<uint8_t*>(ot);
-        constexpr int BS = DC + 16;  // row stride (bytes)
+    if constexpr (PAGED) {
+      if (a.q_low) {  // the 8 further bits: the halves of the wave exchange theirs for 16 adjacent columns each
 #pragma unroll
-        for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int c = cb * 32 + 8 * i + 4 * g;
-            if (c < DC) *reinterpret_cast<uint32_t*>(ob + l32 * BS + c) = low_bits_of(scaled(cb, i));
-          }
-#pragma unroll 4
-        for (int i = lane; i < 32 * (DC / 16); i += 64) {
-          const int t = i / (DC / 16), k = i - t * (DC / 16);
-          if (tok0 + t < Nq)
-            *reinterpret_cast<u32x4*>(a.q_low + ((int64_t)(tok0 + t) * H + h) * DQKP + k * 16) =
-                *reinterpret_cast<const u32x4*>(ob + t * BS + k * 16);
+        for (int cb = 0; cb < NCB; ++cb) {
+          auto swap = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_permlane32_swap(x, y, false, false); };
+          const auto c01 = swap(low_bits_of(scaled(cb, 0)), low_bits_of(scaled(cb, 1)));
+          const auto c23 = swap(low_bits_of(scaled(cb, 2)), low_bits_of(scaled(cb, 3)));
+          const auto lo = swap(c01[0], c23[0]), hi = swap(c01[1], c23[1]);
+          const int c = c0 + cb * 32 + 16 * g;
+          if (ok && c < DC)
+            *reinterpret_cast<u32x4*>(a.q_low + (int64_t)row * DQKP + c) = u32x4{lo[0], hi[0], lo[1], hi[1]};
         }
-        asm volatile("" : "+s"(scale));  // the products are taken again: kept, they would cost a wave per SIMD
       }
     }
     if (ok || STAGE) {
@@ -200,7 +192,7 @@ __global__ __launch_bounds__(256) void q_absorb_kernel(const Args a) {
             const f32x4 v = scaled(cb, i);
             *reinterpret_cast<bf16x4*>(STAGE ? ot + l32 * OS + c : dst + c) = to_bf16x4(v);
             if constexpr (PAGED) {
-              if (ok && (!STAGE || a.q_lo)) paged_q_lo(a, (int64_t)row * DQKP + c, v);
+              if (ok && a.q_lo) *reinterpret_cast<bf16x4*>(a.q_lo + (int64_t)row * DQKP + c) = second_term_of(v);
             }
           }
         }

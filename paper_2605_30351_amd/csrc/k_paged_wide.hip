@@ -245,12 +245,7 @@ __global__ __launch_bounds__(NW * 64, 1) void paged_attend_wide_kernel(const Pag
 
     float q2 = 0.f;  // the squared length of this lane's query
 #pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks) {
-      const bf16x2 h[4] = {__builtin_shufflevector(q[ks], q[ks], 0, 1), __builtin_shufflevector(q[ks], q[ks], 2, 3),
-                           __builtin_shufflevector(q[ks], q[ks], 4, 5), __builtin_shufflevector(q[ks], q[ks], 6, 7)};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q2 = __builtin_amdgcn_fdot2_f32_bf16(h[i], h[i], q2, false);
-    }
+    for (int ks = 0; ks < C::KS; ++ks) q2 = add_squares(q[ks], q2);
     const bool long_row = __builtin_amdgcn_ballot_w64(half_swap_sum(q2) > kOneTerm * kOneTerm) != 0;
     auto fetch_lo = [&]() {
       const int ln = lane_here(), r = row0 + (ln & 31);

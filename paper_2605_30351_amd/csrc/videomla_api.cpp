@@ -1096,7 +1096,7 @@ PagedLayout paged_layout(const videomla_dims* d, const videomla_paged* p, int64_
     return off;
   };
   L.qcat = take((size_t)rows * qk * 2);
-  L.q_lo = L.unit == 32 && d->d_c == 512 ? 0 : take((size_t)rows * qk * (L.unit == 32 ? 1 : 2));
+  L.q_lo = take((size_t)rows * qk * (L.unit == 32 ? 1 : 2));
   L.o_lat = take((size_t)rows * d->d_c * 4);
   L.o_part = take((size_t)2 * L.n_wg * L.rows * d->d_c * 4);
   L.ml = take((size_t)2 * L.n_wg * L.rows * 2 * 4);
@@ -1171,7 +1171,7 @@ int videomla_paged_attend(const videomla_dims* d, const videomla_paged* p, const
   a.q_nope = q_nope; a.q_r = q_r; a.w_uk = w_uk; a.w_uv = w_uv; a.c_kv = c_kv; a.k_r = k_r; a.out = out;
   a.qcat = reinterpret_cast<uint16_t*>(ws + L.qcat);
   a.q_lo = L.unit != 32 ? reinterpret_cast<uint16_t*>(ws + L.q_lo) : nullptr;
-  a.q_low = L.unit == 32 && L.q_lo ? reinterpret_cast<uint8_t*>(ws + L.q_lo) : nullptr;
+  a.q_low = L.unit == 32 ? reinterpret_cast<uint8_t*>(ws + L.q_lo) : nullptr;
   a.o_lat = reinterpret_cast<float*>(ws + L.o_lat);
   a.o_part = reinterpret_cast<float*>(ws + L.o_part);
   a.ml_part = reinterpret_cast<float*>(ws + L.ml);

@@ -204,8 +204,10 @@ __device__ __forceinline__ uint32_t not_finite_keys(At chunk_at) {
   const int lane = lane_here();
   uint64_t bad = 0;
 #pragma unroll 1
-  for (int c = 0; c < CHUNKS; c += 2)
-    bad |= __builtin_amdgcn_ballot_w64(not_finite(*reinterpret_cast<const u32x4*>(chunk_at(lane & 31, c + (lane >> 5)))));
+  for (int c = 0; c < CHUNKS; c += 2) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(chunk_at(lane & 31, c + (lane >> 5)));
+    bad |= __builtin_amdgcn_ballot_w64(not_finite(v));
+  }
   return (uint32_t)bad | (uint32_t)(bad >> 32);
 }
 
@@ -307,24 +309,36 @@ struct PagedAttendArgs : AttendArgs {
   PagedGeo pg;
   PagedPlan plan;
   uint16_t* q_lo;      // workspace: q_cat's second bf16 term, q_cat - bf16(q_cat), for the few-row kernel, or nullptr
-  uint8_t* q_low;      // workspace: the same in 8 bits (low_bits_of), for the wide kernel, or nullptr
+  uint8_t* q_low;      // workspace: the same in 8 bits (low_bits_of), for the kernels of many rows, or nullptr
   float* o_lat;        // workspace: [n_tokens * H][d_c] fp32, rows of unsplit blocks
   int32_t max_blocks;  // row blocks the plan holds
   int32_t rows, unit;  // rows per block, keys per unit
   int32_t cost;        // counts of a block beyond its units
 };
 
-// The wide kernel multiplies the second term of q_cat where one alone would be off by more than about the output's
-// own rounding: where a block has a row longer than kOneTerm (against keys of unit RMS: the standard deviation of
-// its scores, in exponents of 2) and, of whatever scale queries and keys are, where the scores of some row are
-// further apart than kSpread in the first tile of a workgroup's part of a block, or in a later one that raises a
-// running maximum, as those of larger keys do: then it takes its part again from the start. Of 256 rows one is
-// found in the first tile if their deviation is 3 or more; at 1.4, of a plain softmax over unit vectors, none in
-// 10^6 tiles is.
+// The kernels of many rows multiply the second term of q_cat where one alone would be off by more than about the
+// output's own rounding: where a block has a row longer than kOneTerm (against keys of unit RMS: the standard
+// deviation of its scores, in exponents of 2) and, of whatever scale queries and keys are, where the scores of some
+// row are further apart than kSpread in the first tile of a workgroup's part of a block, or in a later one that
+// raises a running maximum, as those of larger keys do: then it takes its part again from the start. Of 256 rows
+// one is found in the first tile if their deviation is 3 or more; at 1.4, of a plain softmax over unit vectors,
+// none in 10^6 tiles is.
 constexpr float kOneTerm = 2.3f, kSpread = 10.f;
 
+// sum + the squares of 8 values.
+__device__ __forceinline__ float add_squares(bf16x8 v, float sum) {
+  const u32x4 u = as_u32x4(v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = u[i];
+    const bf16x2 h = __builtin_bit_cast(bf16x2, w);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(h, h, sum, false);
+  }
+  return sum;
+}
+
 // The second bf16 term of four values of q_cat (their first has been, or is, rounded from them). The few-row
-// kernel reads it as it is. For the wide kernel, which seldom does, the absorption writes half the bytes: the
+// kernel reads it as it is. For the kernels of many rows, which seldom do, the absorption writes half the bytes: the
 // 8 bits of the value that follow its first term's, as the signed distance from it in steps of the float's bit
 // pattern (of 2^-8 of the first term's last place).
 __device__ __forceinline__ bf16x4 second_term_of(f32x4 v) {

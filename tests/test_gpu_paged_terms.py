@@ -15,7 +15,7 @@ from tests.test_gpu_paged import TEXT, attend  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
-WIDTHS = [TEXT.replace(d_c=n, n_heads=12) for n in (64, 128, 192, 256)]
+WIDTHS = [TEXT.replace(d_c=n, n_heads=12) for n in (64, 128, 192, 256, 512)]
 
 
 def scaled(bits, factor):
