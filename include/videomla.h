@@ -432,7 +432,8 @@ int videomla_dense_attend(const videomla_dims* dims, const videomla_window* win,
  * The arrays are read by the kernels: a captured graph replays with the lengths, positions and pages
  * that they hold then. Values out of range are clamped (lengths to what the table can name, offsets to
  * the rows), so that none of them makes a call leave its buffers. Two rows that name the same place of
- * the pool in one write leave either of the two; everything else in the pool stays as it is.
+ * the pool in one write leave a mixture there, each 16 bytes of it from either of the two; everything else
+ * in the pool stays as it is.
  */
 typedef struct videomla_paged {
   int32_t n_seqs, n_tokens, page_tokens, max_pages, n_pages, max_new;
