@@ -658,9 +658,9 @@ constexpr int few_most(int dc) { return dc <= 192 ? 2 : 1; }
 }  // namespace
 
 void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit, int32_t* cost) {
-  const int wide = paged_wide_rows(d_c, d_rope), most = 16 * few_most(d_c);
-  if (wide > 0 && max_rows > most) {
-    *rows = wide;
+  const int most = 16 * few_most(d_c);
+  if (max_rows > most) {
+    *rows = paged_wide_rows(d_c, d_rope);
     *unit = 32;
     *cost = 8;
     return;

@@ -428,8 +428,7 @@ int paged_wide_rows(int d_c, int d_rope) {
 #define X(DC, DR) if (d_c == DC && d_rope == DR) return 32 * wide_waves(DC);
   VMLA_PAGED_WIDE_SHAPES(X)
 #undef X
-  if (d_c == 512 && d_rope == 32) return 64;  // k_paged_wide512.hip
-  return 0;
+  return 64;  // d_c = 512
 }
 
 hipError_t launch_paged_attend_wide(const PagedAttendArgs& a, hipStream_t s) {

@@ -46,8 +46,9 @@ struct PagedSeq {
   int64_t first;
 };
 
-// Element i of an array that no kernel of the call writes; with UNIFORM (i the same in all lanes) by a
-// scalar load, which does not wait for the vector loads in flight.
+// Element i of an array that no workgroup of the same launch writes (the scalar cache, which earlier launches'
+// writes do reach, would not see its); with UNIFORM (i the same in all lanes) by a scalar load, which does not
+// wait for the vector loads in flight.
 template <bool UNIFORM, class T>
 __device__ __forceinline__ T paged_read(const T* p, int64_t i) {
   if constexpr (UNIFORM && !std::is_integral<T>::value) {
@@ -288,10 +289,6 @@ struct alignas(8) PagedRow {  // (one store: rows that bad offsets give to two b
   int32_t w0;
   uint16_t ns, row;
 };
-// The workgroup that takes count u of U, split over G.
-__device__ __forceinline__ int paged_owner(int64_t u, int64_t U, int64_t G) {
-  return (int)floor_div((u + 1) * G - 1, U);
-}
 
 struct PagedPlan {
   int64_t* first;         // [max_blocks] first count of each block
@@ -391,7 +388,7 @@ hipError_t launch_paged_out(const PagedAttendArgs& a, hipStream_t s);
 
 // Rows per block and keys per unit of the attention kernel for sequences of at most max_rows rows.
 void paged_attend_shape(int d_c, int d_rope, int64_t max_rows, int32_t* rows, int32_t* unit, int32_t* cost);
-// The kernel of many rows per block (k_paged_wide.hip): its block, 0 where it is not built, and launch.
+// The kernels of many rows per block (k_paged_wide.hip, for d_c = 512 k_paged_wide512.hip): rows, and launch.
 int paged_wide_rows(int d_c, int d_rope);
 hipError_t launch_paged_attend_wide(const PagedAttendArgs& a, hipStream_t s);
 hipError_t launch_paged_attend_wide512(const PagedAttendArgs& a, hipStream_t s);

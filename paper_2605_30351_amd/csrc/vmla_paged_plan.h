@@ -114,7 +114,8 @@ __device__ __forceinline__ void paged_plan(const PagedAttendArgs& a, void* lds) 
       const PagedBlock p = a.plan.block[lo];
       k.end = (int32_t)(u1 - at);
       k.n = (int32_t)(u1 - u);
-      k.last_ns = paged_owner(at + a.cost + p.n_units - 1, units, G) - paged_owner(at + a.cost, units, G) + 1;
+      k.last_ns = attend_owner(at + a.cost + p.n_units - 1, units, (int)G) -
+                  attend_owner(at + a.cost, units, (int)G) + 1;
       a.plan.work_block[w] = p;
     }
     a.plan.work[w] = k;
