@@ -1062,8 +1062,8 @@ PagedGeo make_paged_geo(const videomla_dims* d, const videomla_paged* p) {
   return g;
 }
 
-// Workspace of a paged attention call: q_cat and o_lat rows, the partial results of 2 n_wg slots and
-// the plan.
+// Workspace of a paged attention call: q_cat with its second terms, o_lat rows, the partial results of 2 n_wg
+// slots and the plan.
 struct PagedLayout {
   size_t qcat, q_lo, o_lat, o_part, ml, row, block, first, work, work_block, total;
   int32_t rows, unit, cost, max_blocks, n_wg;
